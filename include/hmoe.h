@@ -57,7 +57,7 @@ enum {
   HMOE_ERR_HIP = -6
 };
 
-enum { HMOE_F32 = 0, HMOE_BF16 = 1, HMOE_BF16_W4 = 2 };
+enum { HMOE_F32 = 0, HMOE_BF16 = 1, HMOE_BF16_W4 = 2, HMOE_BF16_I8 = 3 };
 
 /*
  * HMOE_BF16_W4: activations bfloat16 as for HMOE_BF16, expert weights stored in 4 bits (the paper runs
@@ -69,6 +69,20 @@ enum { HMOE_F32 = 0, HMOE_BF16 = 1, HMOE_BF16_W4 = 2 };
  * H % 128 == 0 and F % 128 == 0.  FFN paths: HMOE_FFN_SKINNY (AUTO up to 16 tokens), HMOE_FFN_TILED
  * (AUTO above) and HMOE_FFN_REFERENCE.  Everything else (router, route, permute, combine) behaves as for
  * HMOE_BF16.
+ */
+
+/*
+ * HMOE_BF16_I8: activations bfloat16 as for HMOE_BF16, the experts' three products in 8-bit integers with one scale per
+ * token and one per output channel.  A row v (of a weight matrix W [N, K], of the tokens, of the intermediate h) becomes
+ *     amax = max(max_k |v_k|, 2^-100)   s = amax / 127   q_k = rint(127 v_k / amax), in -127 .. 127   (fp32, nearest even)
+ * and a product of a token row and a weight row is s_token * s_weight * sum_k q_k q'_k, the sum in 32-bit integers
+ * (exact: H and F are at most 131072).  hmoe_pack_expert quantises bfloat16 weights; tokens are quantised inside the FFN
+ * calls; h = silu(g) * u stays in fp32 and is quantised row by row, a row being the F values of one assignment; outputs
+ * are rounded to bfloat16 once.  A row of zeros has codes 0; a row that holds an infinity or a NaN makes every result that
+ * it takes part in NaN.  The sums being exact, results do not depend on the number of tokens or the path beyond the last
+ * bits of silu (HMOE_FFN_REFERENCE divides and takes expf).
+ * Needs H % 128 == 0 and F % 128 == 0.  FFN paths: HMOE_FFN_SKINNY (AUTO up to 32 tokens), HMOE_FFN_TILED (AUTO above) and
+ * HMOE_FFN_REFERENCE.  Everything else (router, route, permute, combine) behaves as for HMOE_BF16.
  */
 
 /* Which FFN kernels hmoe_expert_ffn_grouped uses.  AUTO picks by token count. */
@@ -90,7 +104,7 @@ typedef struct hmoe_layer_desc {
   int32_t n_experts; /* E, 1..HMOE_MAX_EXPERTS                     */
   int32_t top_k;     /* K, 1..min(E, HMOE_MAX_TOP_K)               */
   int32_t n_slots;   /* S, 1..E                                    */
-  int32_t dtype;     /* HMOE_F32, HMOE_BF16 or HMOE_BF16_W4        */
+  int32_t dtype;     /* HMOE_F32, HMOE_BF16, HMOE_BF16_W4 or HMOE_BF16_I8 */
 } hmoe_layer_desc;
 
 /* Host-side cache object: slot table mirror, use ticks, events.  Opaque. */
@@ -291,7 +305,8 @@ int32_t hmoe_route_scores(const hmoe_layer_desc* desc, const float* logits, int3
  *       expert.  An expert named here that is not resident (host mirror) ->
  *       HMOE_ERR_NOT_RESIDENT, nothing enqueued.  Rows of experts that are not active or not
  *       resident are left untouched.
- *   workspace: hmoe_ffn_workspace_bytes(desc, A) bytes of device scratch (holds h [A, F]).
+ *   workspace: hmoe_ffn_workspace_bytes(desc, A) bytes of device scratch (holds h [A, F]; for HMOE_BF16_I8 h in fp32, the
+ *       codes of the rows at hand and their scales).
  *   path: HMOE_FFN_*; AUTO = SKINNY when T = A/K <= 32 (4-bit weights: 16) else TILED; for fp32 tiles of their own
  *       when H and F are multiples of 4 and there are more than a few rows, else REFERENCE (the only path by name).
  * Shared experts (Section II-A) use the same call with a 1-expert layer (E = K = S = 1,
@@ -340,6 +355,49 @@ int32_t hmoe_expert_ffn_grouped_with_shared(
  */
 int32_t hmoe_combine(const hmoe_layer_desc* desc, const void* o_perm, const int32_t* inv_perm,
                      const float* topk_w, const void* o_shared, int32_t T, void* y, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Gradients of the layer around its experts, for training the router (over experts that stay as they are, quantised ones
+ * among them) and for callers that bring the gradient of the expert FFN itself.  With dy = dL/dy [T, H]:
+ *     hmoe_combine_backward  dy -> d_o_perm (the experts' outputs) and d_topk_w (the gate weights); dL/d(o_shared) is dy
+ *     hmoe_permute_backward  d_x_perm (the experts' inputs, sorted) -> dx
+ *     hmoe_route_backward    d_topk_w -> d_logits
+ *     hmoe_router_backward   d_logits -> dx and d_w_g
+ * Activations, weights and their gradients have the layer's activation type (fp32, or bfloat16 for every other dtype);
+ * gate weights, logits and d_w_g are fp32.  Sums are fp32 in a fixed order: no atomics, the same bits every time.  T = 0 is
+ * a no-op (hmoe_router_backward still writes d_w_g: zeros).  bfloat16 rows need H % 8 == 0 (hmoe_router_backward H % 16).
+ *
+ * hmoe_combine_backward: the gradient of hmoe_combine.  For every assignment a = t*K + j at sorted row p = inv_perm[a]:
+ *     d_o_perm[p] = topk_w[t, j] * dy[t]      (one rounding)
+ *     d_topk_w[t, j] = sum_h dy[t, h] * o_perm[p, h]
+ *   o_perm, inv_perm, topk_w as hmoe_combine had them.  Either result may be NULL; o_perm may be NULL without d_topk_w, topk_w
+ *   without d_o_perm.  d_o_perm may be o_perm itself.  An assignment whose inv_perm is outside [0, T*K) has no row:
+ *   its d_topk_w is 0.
+ *
+ * hmoe_permute_backward: the gradient of hmoe_permute's row gather (and of the gather inside the FFN calls):
+ *     dx[t] = sum_{j<K} d_x_perm[inv_perm[t*K + j]] (+ add[t])
+ *   j in ascending order, then `add` [T, H] (or NULL: what reaches x on other ways, the shared experts' gradient say);
+ *   fp32 accumulation, one rounding.  dx may be `add` itself.
+ *
+ * hmoe_route_backward: the gradient of hmoe_route's softmax over the chosen logits (the choice itself has none):
+ *     d_logits[t, topk_idx[t, j]] = topk_w[t, j] * (d_topk_w[t, j] - sum_i topk_w[t, i] * d_topk_w[t, i]), other entries 0
+ *   topk_idx, topk_w as written by hmoe_route; an id that a token names twice gets the sum, one outside [0, E) none.
+ *
+ * hmoe_router_backward: the gradient of hmoe_router_logits.  d_logits [T, E] is dense (a caller may have added to it):
+ *     dx[t]    = sum_e d_logits[t, e] * w_g[e] (+ add[t])
+ *     d_w_g[e] = sum_t d_logits[t, e] * x[t]          fp32
+ *   Either result may be NULL, then what only it needs may be NULL too; dx may be `add` itself, no other two may overlap.
+ *   workspace: hmoe_router_backward_workspace_bytes(desc, T) bytes of device scratch, 16-byte aligned.
+ */
+int32_t hmoe_combine_backward(const hmoe_layer_desc* desc, const void* dy, const void* o_perm, const int32_t* inv_perm,
+                              const float* topk_w, int32_t T, void* d_o_perm, float* d_topk_w, void* stream);
+int32_t hmoe_permute_backward(const hmoe_layer_desc* desc, const void* d_x_perm, const int32_t* inv_perm, int32_t T,
+                              const void* add, void* dx, void* stream);
+int32_t hmoe_route_backward(const hmoe_layer_desc* desc, const int32_t* topk_idx, const float* topk_w, const float* d_topk_w,
+                            int32_t T, float* d_logits, void* stream);
+size_t hmoe_router_backward_workspace_bytes(const hmoe_layer_desc* desc, int32_t T);
+int32_t hmoe_router_backward(const hmoe_layer_desc* desc, const void* x, const void* w_g, const float* d_logits, int32_t T,
+                             const void* add, void* dx, float* d_w_g, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Grouped expert FFN over a cache that holds fewer experts than the call needs (on-demand loading of the missing

@@ -31,6 +31,7 @@ HMOE_ERR_HIP = -6
 HMOE_F32 = 0
 HMOE_BF16 = 1
 HMOE_BF16_W4 = 2      # bf16 activations, 4-bit group-wise expert weights
+HMOE_BF16_I8 = 3      # bf16 activations, experts' products in 8-bit integers with a scale per token and output channel
 HMOE_FFN_AUTO, HMOE_FFN_REFERENCE, HMOE_FFN_SKINNY, HMOE_FFN_TILED = 0, 1, 2, 3
 
 # every symbol include/hmoe.h declares
@@ -43,7 +44,8 @@ EXPORTS = [
     "hmoe_router_route_permute", "hmoe_expert_ffn_grouped_with_shared", "hmoe_ffn_combine_sync_bytes", "hmoe_expert_ffn_combine",
     "hmoe_route_ffn_combine", "hmoe_layer_forward",
     "hmoe_expert_ffn_staged",
-    "hmoe_combine",
+    "hmoe_combine", "hmoe_combine_backward", "hmoe_permute_backward", "hmoe_route_backward",
+    "hmoe_router_backward_workspace_bytes", "hmoe_router_backward",
     "hmoe_cache_set_policy", "hmoe_cache_update_scores", "hmoe_cache_get_scores", "hmoe_cache_set_layer",
     "hmoe_route_scores_workspace_bytes", "hmoe_route_scores",
     "hmoe_schedule_simulate", "hmoe_schedule_plan",
@@ -130,6 +132,12 @@ def _load() -> ctypes.CDLL:
     lib.hmoe_route_permute.argtypes = [dp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hmoe_router_route_permute.argtypes = [dp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hmoe_combine.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp]
+    lib.hmoe_combine_backward.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.hmoe_permute_backward.argtypes = [dp, vp, vp, i32, vp, vp, vp]
+    lib.hmoe_route_backward.argtypes = [dp, vp, vp, vp, i32, vp, vp]
+    lib.hmoe_router_backward_workspace_bytes.restype = sz
+    lib.hmoe_router_backward_workspace_bytes.argtypes = [dp, i32]
+    lib.hmoe_router_backward.argtypes = [dp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.hmoe_cache_set_policy.argtypes = [vp, i32, ctypes.c_float]
     lib.hmoe_cache_set_layer.argtypes = [vp, dp]
     lib.hmoe_cache_update_scores.argtypes = [vp, vp, i32]
@@ -367,6 +375,34 @@ def hmoe_router_route_permute(desc, x, w_g, T, logits, topk_idx, topk_w, expert_
 def hmoe_combine(desc, o_perm, inv_perm, topk_w, o_shared, T, y, stream=None):
     _check(_lib.hmoe_combine(ctypes.byref(desc), _ptr(o_perm), _ptr(inv_perm), _ptr(topk_w), _ptr(o_shared), T,
                              _ptr(y), _stream(stream)), "hmoe_combine")
+
+
+def hmoe_combine_backward(desc, dy, o_perm, inv_perm, topk_w, T, d_o_perm, d_topk_w, stream=None):
+    """Gradient of hmoe_combine: dy [T, H] -> d_o_perm [T*K, H] and / or d_topk_w [T, K] (None leaves a result out)."""
+    _check(_lib.hmoe_combine_backward(ctypes.byref(desc), _ptr(dy), _ptr(o_perm), _ptr(inv_perm), _ptr(topk_w), T,
+                                      _ptr(d_o_perm), _ptr(d_topk_w), _stream(stream)), "hmoe_combine_backward")
+
+
+def hmoe_permute_backward(desc, d_x_perm, inv_perm, T, add, dx, stream=None):
+    """Gradient of the row gather: d_x_perm [T*K, H] -> dx [T, H] (+ add [T, H] or None)."""
+    _check(_lib.hmoe_permute_backward(ctypes.byref(desc), _ptr(d_x_perm), _ptr(inv_perm), T, _ptr(add), _ptr(dx),
+                                      _stream(stream)), "hmoe_permute_backward")
+
+
+def hmoe_route_backward(desc, topk_idx, topk_w, d_topk_w, T, d_logits, stream=None):
+    """Gradient of the gates: d_topk_w [T, K] -> d_logits [T, E]."""
+    _check(_lib.hmoe_route_backward(ctypes.byref(desc), _ptr(topk_idx), _ptr(topk_w), _ptr(d_topk_w), T, _ptr(d_logits),
+                                    _stream(stream)), "hmoe_route_backward")
+
+
+def hmoe_router_backward_workspace_bytes(desc, T) -> int:
+    return int(_lib.hmoe_router_backward_workspace_bytes(ctypes.byref(desc), T))
+
+
+def hmoe_router_backward(desc, x, w_g, d_logits, T, add, dx, d_w_g, workspace, workspace_bytes, stream=None):
+    """Gradient of hmoe_router_logits: d_logits [T, E] -> dx [T, H] (+ add or None) and / or d_w_g [E, H] fp32."""
+    _check(_lib.hmoe_router_backward(ctypes.byref(desc), _ptr(x), _ptr(w_g), _ptr(d_logits), T, _ptr(add), _ptr(dx),
+                                     _ptr(d_w_g), _ptr(workspace), workspace_bytes, _stream(stream)), "hmoe_router_backward")
 
 
 def hmoe_cache_set_layer(cache, routed_desc):

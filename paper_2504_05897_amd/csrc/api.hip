@@ -39,7 +39,8 @@ int check_desc(const hmoe_layer_desc* d) {
   if (d->hidden <= 0 || d->ffn <= 0 || d->n_experts <= 0 || d->top_k <= 0 || d->n_slots <= 0)
     return HMOE_ERR_INVALID_ARG;
   if (d->top_k > d->n_experts || d->n_slots > d->n_experts) return HMOE_ERR_INVALID_ARG;
-  if (d->dtype != HMOE_F32 && d->dtype != HMOE_BF16 && d->dtype != HMOE_BF16_W4) return HMOE_ERR_INVALID_ARG;
+  if (d->dtype != HMOE_F32 && d->dtype != HMOE_BF16 && d->dtype != HMOE_BF16_W4 && d->dtype != HMOE_BF16_I8)
+    return HMOE_ERR_INVALID_ARG;
   if (d->n_experts > HMOE_MAX_EXPERTS || d->top_k > HMOE_MAX_TOP_K) return HMOE_ERR_UNSUPPORTED;
   return HMOE_OK;
 }
@@ -49,6 +50,8 @@ static int check_ffn_shape(const hmoe_layer_desc* d) {
   if (rc != HMOE_OK) return rc;
   if (d->dtype == HMOE_BF16 && (d->hidden % 64 != 0 || d->ffn % 64 != 0)) return HMOE_ERR_UNSUPPORTED;
   if (d->dtype == HMOE_BF16_W4 && (d->hidden % W4_GROUP != 0 || d->ffn % W4_GROUP != 0)) return HMOE_ERR_UNSUPPORTED;
+  if (d->dtype == HMOE_BF16_I8 &&
+      (d->hidden % I8_K_UNIT != 0 || d->ffn % I8_K_UNIT != 0 || d->hidden > I8_MAX_K || d->ffn > I8_MAX_K)) return HMOE_ERR_UNSUPPORTED;
   return HMOE_OK;
 }
 
@@ -126,6 +129,10 @@ extern "C" size_t hmoe_slot_bytes(const hmoe_layer_desc* desc) {
     if (check_ffn_shape(desc) != HMOE_OK) return 0;
     return w4_offsets((size_t)desc->hidden, (size_t)desc->ffn).total;  // a multiple of 256 for valid shapes
   }
+  if (desc->dtype == HMOE_BF16_I8) {
+    if (check_ffn_shape(desc) != HMOE_OK) return 0;
+    return i8_offsets((size_t)desc->hidden, (size_t)desc->ffn).total;  // likewise
+  }
   const size_t elem = desc->dtype == HMOE_BF16 ? 2 : 4;
   const size_t raw = 3 * (size_t)desc->hidden * desc->ffn * elem;
   return (raw + 255) & ~(size_t)255;
@@ -171,6 +178,33 @@ static void quantize_matrix_w4(const bf16_t* src, int N, int K, uint32_t* units,
   }
 }
 
+// ---- 8-bit quantisation (host) ------------------------------------------------------------
+// One row of bfloat16 values -> its codes at their places in the packed matrix (row packed_n); returns the row's scale.
+// 127 v is exact in fp32 and the quotient the only rounding before rint, so a value halfway between two codes is seen as
+// such (rows of very large values are scaled by a power of two first, or 127 v could overflow).  Written to vectorise: the
+// magnitudes' maximum is that of their bit patterns, and adding 1.5 * 2^23 leaves no bits behind the point (nearest even).
+static float quantize_row_i8(const bf16_t* src, int K, char* packed, int packed_n) {
+  int16_t largest = 0;
+  for (int k = 0; k < K; ++k) largest = std::max(largest, (int16_t)(src[k] & 0x7fff));
+  const bool finite = largest < 0x7f80;  // else the scale carries the infinity or NaN into every result
+  const float amax = finite ? std::max(bf16_bits_to_f32((bf16_t)largest), I8_MIN_AMAX) : 1.0f;
+  const float down = amax > 0x1p100f ? 0x1p-10f : 1.0f, times = 127.0f * down, by = amax * down;
+  for (int k = 0; k < K; k += 16) {
+    int8_t codes[16];
+    for (int i = 0; i < 16; ++i) {
+      const float q = times * bf16_bits_to_f32(src[k + i]) / by + 12582912.0f;
+      codes[i] = finite ? (int8_t)(int)(q - 12582912.0f) : (int8_t)0;
+    }
+    memcpy(packed + i8_packed_index(packed_n, k, K), codes, 16);
+  }
+  return finite ? amax / 127.0f : std::nanf("");
+}
+// src [N, K] -> packed codes and scales; source rows [32 q, 32 q + 32) are packed group q * stride + first
+static void quantize_matrix_i8(const bf16_t* src, int N, int K, char* packed, float* scales, int stride, int first) {
+  for (int n = 0; n < N; ++n)
+    scales[n] = quantize_row_i8(src + (size_t)n * K, K, packed, (n / TILE_N * stride + first) * TILE_N + n % TILE_N);
+}
+
 // rows [n0, n0+32) of src [*, K] -> one 32-row group of tiles at dst
 static void pack_row_group(const bf16_t* src, int n0, int K, bf16_t* dst) {
   const int kt = K / TILE_K;
@@ -204,6 +238,14 @@ extern "C" int32_t hmoe_pack_expert(const hmoe_layer_desc* desc, const void* h_w
     quantize_matrix_w4((const bf16_t*)h_w_up, (int)F, (int)H, (uint32_t*)base, (bf16_t*)(base + off.gate_up_scales), 2, 1);
     quantize_matrix_w4((const bf16_t*)h_w_down, (int)H, (int)F, (uint32_t*)(base + off.down_units),
                        (bf16_t*)(base + off.down_scales), 1, 0);
+    return HMOE_OK;
+  }
+  if (desc->dtype == HMOE_BF16_I8) {
+    const I8Offsets off = i8_offsets(H, F);
+    char* base = (char*)h_packed_out;
+    quantize_matrix_i8((const bf16_t*)h_w_gate, (int)F, (int)H, base, (float*)(base + off.gate_scales), 2, 0);
+    quantize_matrix_i8((const bf16_t*)h_w_up, (int)F, (int)H, base, (float*)(base + off.up_scales), 2, 1);
+    quantize_matrix_i8((const bf16_t*)h_w_down, (int)H, (int)F, base + off.down, (float*)(base + off.down_scales), 1, 0);
     return HMOE_OK;
   }
   bf16_t* out = (bf16_t*)h_packed_out;
@@ -446,6 +488,7 @@ extern "C" int32_t hmoe_cache_get_scores(const hmoe_cache* c, double* h_out) {
 // ---- FFN dispatch ------------------------------------------------------------------------
 extern "C" size_t hmoe_ffn_workspace_bytes(const hmoe_layer_desc* desc, int32_t A) {
   if (check_desc(desc) != HMOE_OK || A < 0) return 0;
+  if (desc->dtype == HMOE_BF16_I8) return i8_work((size_t)A, (size_t)desc->hidden, (size_t)desc->ffn).total;
   const size_t elem = desc->dtype == HMOE_F32 ? 4 : 2;
   return (((size_t)A * desc->ffn * elem) + 255) & ~(size_t)255;
 }
@@ -487,6 +530,7 @@ static int32_t ffn_prepare(const hmoe_layer_desc* desc, hmoe_cache* cache, const
   a.stream = (hipStream_t)stream;
   a.beside = cache->has_beside ? &cache->beside : nullptr;
   memset(&a.active, 0, sizeof(a.active));
+  a.all_active = !h_active;
   if (h_active) {
     for (int i = 0; i < n_active; ++i) {
       const int e = h_active[i];
@@ -512,6 +556,7 @@ static int32_t ffn_prepare(const hmoe_layer_desc* desc, hmoe_cache* cache, const
 }
 
 static int32_t ffn_launch(const FfnArgs& a, int32_t path) {
+  if (a.desc->dtype == HMOE_BF16_I8) return launch_ffn_reference_i8(a);
   if (path == FFN_F32_TILES) return launch_ffn_f32(a);
   if (path == HMOE_FFN_REFERENCE) return launch_ffn_reference(a);
   if (path == HMOE_FFN_SKINNY) return a.desc->dtype == HMOE_BF16_W4 ? launch_ffn_skinny_w4(a) : launch_ffn_skinny(a);

@@ -2,6 +2,7 @@
 //   y[t] = sum_{j<K} w[t,j] * o_perm[inv_perm[t*K+j]] (+ o_shared[t]),
 // j ascending then the shared term, fp32 accumulation, one rounding.  No atomics: every output
 // element is produced by one lane, so results do not depend on scheduling.
+// hmoe_permute_backward is the same sum without weights: the gradient of the row gather.
 // Also: hmoe_router_logits (x . W_g), the small GEMM in front of the router.
 #include "router_body.h"
 
@@ -35,10 +36,11 @@ __device__ __forceinline__ void combine_store(uint4* y, const float (&acc)[8]) {
 __device__ __forceinline__ void combine_store(float4* y, const float (&acc)[4]) { *y = make_float4(acc[0], acc[1], acc[2], acc[3]); }
 
 // VEC: 16 bytes, N elements.  K: experts per token (exact up to 8), or 8 at a time of top_k.  STREAM: non-temporal loads.
-template <class VEC, int N, int K, bool EXACT, bool SHARED, bool STREAM>
+// WEIGHTED: by topk_w, else every weight is 1.  (y may be o_shared, which a thread reads before it stores in the same place.)
+template <class VEC, int N, int K, bool EXACT, bool SHARED, bool STREAM, bool WEIGHTED>
 __global__ __launch_bounds__(256) void combine_kernel(const VEC* __restrict__ o_perm, const int32_t* __restrict__ inv_perm,
-                                                      const float* __restrict__ topk_w, const VEC* __restrict__ o_shared,
-                                                      int top_k, int row_vec, VEC* __restrict__ y) {
+                                                      const float* __restrict__ topk_w, const VEC* o_shared, int top_k,
+                                                      int row_vec, VEC* y) {
   const long t = blockIdx.x;
   const int c = blockIdx.y * blockDim.x + threadIdx.x;
   if (c >= row_vec) return;
@@ -58,13 +60,13 @@ __global__ __launch_bounds__(256) void combine_kernel(const VEC* __restrict__ o_
     }
 #pragma unroll
     for (int j = 0; j < K; ++j)
-      if (EXACT || j0 + j < top_k) combine_add(acc, v[j], w[EXACT ? j : j0 + j]);
+      if (EXACT || j0 + j < top_k) combine_add(acc, v[j], WEIGHTED ? w[EXACT ? j : j0 + j] : 1.0f);
   }
   if (SHARED) combine_add(acc, shared, 1.0f);
   combine_store(&y[t * row_vec + c], acc);
 }
 
-template <class VEC, int N>
+template <class VEC, int N, bool WEIGHTED = true>
 static void launch_combine(const VEC* o_perm, const int32_t* inv_perm, const float* topk_w, const VEC* o_shared, int T, int top_k,
                            int row_vec, VEC* y, hipStream_t s) {
   // A few tokens: blocks of one wave, spread over the CUs.
@@ -79,8 +81,8 @@ static void launch_combine(const VEC* o_perm, const int32_t* inv_perm, const flo
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, o_perm, inv_perm, topk_w, o_shared, top_k, row_vec, y);
   };
 #define HMOE_COMBINE(K, EXACT)                                                                                    \
-  launch(&combine_kernel<VEC, N, K, EXACT, true, false>, &combine_kernel<VEC, N, K, EXACT, false, false>,          \
-         &combine_kernel<VEC, N, K, EXACT, true, true>, &combine_kernel<VEC, N, K, EXACT, false, true>)
+  launch(&combine_kernel<VEC, N, K, EXACT, true, false, WEIGHTED>, &combine_kernel<VEC, N, K, EXACT, false, false, WEIGHTED>, \
+         &combine_kernel<VEC, N, K, EXACT, true, true, WEIGHTED>, &combine_kernel<VEC, N, K, EXACT, false, true, WEIGHTED>)
   switch (top_k) {
     case 1: HMOE_COMBINE(1, true); break;
     case 2: HMOE_COMBINE(2, true); break;
@@ -99,13 +101,12 @@ static void launch_combine(const VEC* o_perm, const int32_t* inv_perm, const flo
 __global__ __launch_bounds__(256) void combine_f32_kernel(const float* __restrict__ o_perm,
                                                           const int32_t* __restrict__ inv_perm,
                                                           const float* __restrict__ topk_w,
-                                                          const float* __restrict__ o_shared, int top_k, int hidden,
-                                                          float* __restrict__ y) {
+                                                          const float* o_shared, int top_k, int hidden, float* y) {
   const long t = blockIdx.x;
   for (int c = threadIdx.x; c < hidden; c += blockDim.x) {
     float acc = 0.0f;
     for (int j = 0; j < top_k; ++j)
-      acc += topk_w[t * top_k + j] * o_perm[(long)inv_perm[t * top_k + j] * hidden + c];
+      acc += (topk_w ? topk_w[t * top_k + j] : 1.0f) * o_perm[(long)inv_perm[t * top_k + j] * hidden + c];
     if (o_shared) acc += o_shared[t * hidden + c];
     y[t * hidden + c] = acc;
   }
@@ -176,6 +177,30 @@ extern "C" int32_t hmoe_combine(const hmoe_layer_desc* desc, const void* o_perm,
   } else {
     hipLaunchKernelGGL(combine_f32_kernel, dim3((unsigned)T), dim3(256), 0, s, (const float*)o_perm, inv_perm, topk_w,
                        (const float*)o_shared, desc->top_k, desc->hidden, (float*)y);
+  }
+  HMOE_HIP(hipGetLastError());
+  return HMOE_OK;
+}
+
+extern "C" int32_t hmoe_permute_backward(const hmoe_layer_desc* desc, const void* d_x_perm, const int32_t* inv_perm, int32_t T,
+                                         const void* add, void* dx, void* stream) {
+  using namespace hmoe;
+  int rc = check_desc(desc);
+  if (rc != HMOE_OK) return rc;
+  if (T < 0 || T > 0x7fffffff / desc->top_k) return HMOE_ERR_INVALID_ARG;
+  if (T == 0) return HMOE_OK;
+  if (!d_x_perm || !inv_perm || !dx) return HMOE_ERR_INVALID_ARG;
+  if (!aligned16(d_x_perm) || !aligned16(dx) || !aligned16(add) || !aligned4(inv_perm)) return HMOE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  const int H = desc->hidden;
+  if (desc->dtype != HMOE_F32) {
+    if (H % 8 != 0) return HMOE_ERR_UNSUPPORTED;
+    launch_combine<uint4, 8, false>((const uint4*)d_x_perm, inv_perm, nullptr, (const uint4*)add, T, desc->top_k, H / 8, (uint4*)dx, s);
+  } else if (H % 4 == 0) {
+    launch_combine<float4, 4, false>((const float4*)d_x_perm, inv_perm, nullptr, (const float4*)add, T, desc->top_k, H / 4, (float4*)dx, s);
+  } else {
+    hipLaunchKernelGGL(combine_f32_kernel, dim3((unsigned)T), dim3(256), 0, s, (const float*)d_x_perm, inv_perm, (const float*)nullptr,
+                       (const float*)add, desc->top_k, H, (float*)dx);
   }
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;

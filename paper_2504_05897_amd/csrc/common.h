@@ -39,6 +39,9 @@ __device__ __forceinline__ bf16_t f32_to_bf16(float f) {
   return (bf16_t)(u >> 16);
 }
 
+// the same for values that may be infinite or NaN (the carry of the rounding turns some NaNs into infinities or zeros)
+__device__ __forceinline__ bf16_t f32_to_bf16_any(float f) { return f != f ? (bf16_t)0x7fc0u : f32_to_bf16(f); }
+
 // two at once: the low half of the result is a, the high half b (same rounding; one instruction on gfx950)
 typedef __bf16 bf16x2_hw_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_hw_t __attribute__((ext_vector_type(2)));
@@ -84,6 +87,7 @@ int set_hip_error(hipError_t err, const char* what);
 int set_error_text(int status, const char* text);  // text for hmoe_last_error; returns status
 int check_desc(const hmoe_layer_desc* d);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // The address under which kernels can write pinned host memory themselves, or NULL (pageable memory, or pinned memory that the
 // device sees elsewhere): a few values then need no copy behind the kernel.
@@ -133,6 +137,45 @@ __host__ __device__ inline size_t w4_scale_index(int n, int group, int n_groups)
   return ((size_t)(n / 16) * n_groups + group) * 16 + n % 16;
 }
 
+// --- 8-bit integer experts (HMOE_BF16_I8) -----------------------------------------------------
+// Codes are packed like bfloat16 weights with two codes in the place of a bfloat16: a tile is 32 rows x 32 k, 1 KiB, in the
+// register order of one 32x32x32 int8 MFMA operand (lane l owns the 16 codes W[32 nb + l % 32][32 kb + 16 (l / 32) .. + 16]).
+// A slot is [gate/up codes: 2F x H, 32-row groups interleaved][down codes: H x F][gate scales F][up scales F][down scales H],
+// the scales fp32.
+constexpr int I8_TILE_K = 32;
+constexpr int I8_K_UNIT = 128;          // H and F are multiples of this
+constexpr int I8_MAX_K = 131072;        // 127 * 127 * 131072 < 2^31: sums of products are exact
+struct I8Offsets {
+  size_t down, gate_scales, up_scales, down_scales, total;  // byte offsets within a slot (gate/up codes at 0)
+};
+__host__ __device__ inline I8Offsets i8_offsets(size_t hidden, size_t ffn) {
+  I8Offsets o;
+  o.down = 2 * hidden * ffn;
+  o.gate_scales = 3 * hidden * ffn;
+  o.up_scales = o.gate_scales + 4 * ffn;
+  o.down_scales = o.up_scales + 4 * ffn;
+  o.total = o.down_scales + 4 * hidden;  // a multiple of 256 for multiples of 128
+  return o;
+}
+// byte offset of the code of packed row n, column k (K columns) within its matrix
+__host__ __device__ inline size_t i8_packed_index(int n, int k, int K) {
+  return ((size_t)(n / TILE_N) * (K / I8_TILE_K) + k / I8_TILE_K) * 1024 + (size_t)(n % TILE_N + TILE_N * (k % I8_TILE_K / 16)) * 16 + k % 16;
+}
+// The smallest amax a row counts with: 127 / amax stays finite, and a row of zeros gets codes 0.
+constexpr float I8_MIN_AMAX = 0x1p-100f;
+// Workspace of an FFN call over A rows: h [A, F] fp32, the codes of the rows that the launch at hand reads ([A, H], then
+// [A, F]: the first are not needed any more when the second are written) and their scales [A].
+struct I8Work {
+  size_t codes, scales, total;  // byte offsets (h at 0)
+};
+inline I8Work i8_work(size_t A, size_t hidden, size_t ffn) {
+  I8Work w;
+  w.codes = (A * ffn * 4 + 255) & ~(size_t)255;
+  w.scales = w.codes + ((A * (hidden > ffn ? hidden : ffn) + 255) & ~(size_t)255);
+  w.total = w.scales + ((A * 4 + 255) & ~(size_t)255);
+  return w;
+}
+
 struct FfnArgs {
   const hmoe_layer_desc* desc = nullptr;
   const void* x_perm = nullptr;       // rows of the gate/up input; with row_map: the un-permuted x [T, H]
@@ -144,6 +187,7 @@ struct FfnArgs {
   const char* slots = nullptr;        // device slot storage
   size_t slot_bytes = 0;
   ActiveMask active = {};
+  bool all_active = true;             // no expert was left out of `active`
   void* o_perm = nullptr;
   void* h = nullptr;                  // workspace [A, F]
   hipStream_t stream = nullptr;
@@ -176,6 +220,7 @@ bool ffn_skinny_routes(const hmoe_layer_desc& d, int T);
 int launch_ffn_tiled(const FfnArgs& a);
 int launch_ffn_skinny_w4(const FfnArgs& a);
 int launch_ffn_tiled_w4(const FfnArgs& a);
+int launch_ffn_reference_i8(const FfnArgs& a);
 
 }  // namespace hmoe
 

@@ -1,0 +1,227 @@
+// Expert FFN in 8-bit integers (HMOE_BF16_I8): what its paths share (quantisation of rows), and the reference path.
+//
+// A call is four launches: the tokens' rows, in sorted order, become codes and scales; gate/up products and SwiGLU leave h in
+// fp32; the rows of h become codes and scales; the down projection rounds to bfloat16.  h cannot be quantised where it is
+// made: the scale of a row is known when its last value is.  It stays in fp32 until then, since a code is decided by where
+// 127 h / amax lies between two halves: 16 bits for it would move one code in a thousand, which is as large an error of the
+// result as its final rounding.
+#include "common.h"
+
+namespace hmoe {
+
+struct I8Ctx {
+  const int32_t* offsets;
+  const int32_t* slot_of;
+  const char* slots;
+  size_t slot_bytes;
+  ActiveMask active;
+  bool all_active;
+  int n_experts, hidden, ffn;
+  const int32_t* row_map;
+  int map_div;
+};
+
+// expert that owns sorted row p: offsets[e] <= p < offsets[e+1]
+__device__ __forceinline__ int i8_expert_of(const int32_t* __restrict__ offsets, int n_experts, int p) {
+  int lo = 0, hi = n_experts;  // invariant: offsets[lo] <= p < offsets[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid] <= p) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// 8 consecutive values of a row as fp32
+__device__ __forceinline__ void load_8(const bf16_t* p, float (&v)[8]) {
+  const u32x4 u = *(const u32x4*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(u[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load_8(const float* p, float (&v)[8]) {
+  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ uint32_t magnitude_bits(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+// What a row's codes are computed with.  bfloat16 rows: 127 v (exact; scaled by a power of two where it could overflow)
+// divided by amax, one rounding, so that halves are seen as such.  fp32 rows, whose values fall on halves by accident only:
+// times the reciprocal, ten instructions fewer per value.
+struct RowQuant {
+  float times, by, scale;
+  bool finite;
+};
+__device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
+  RowQuant q;
+  q.finite = amax_bits < 0x7f800000u;
+  const float amax = q.finite ? fmaxf(__uint_as_float(amax_bits), I8_MIN_AMAX) : 1.0f;
+  const float down = amax > 0x1p100f ? 0x1p-10f : 1.0f;
+  q.times = 127.0f * down;
+  q.by = amax * down;
+  q.scale = q.finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
+  return q;
+}
+template <bool DIVIDE>
+__device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q) {
+  uint32_t w[2] = {0, 0};
+  const float r = DIVIDE ? 0.0f : q.times / q.by;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = DIVIDE ? v[i] * q.times / q.by : v[i] * r;
+    w[i / 4] |= ((uint32_t)__float2int_rn(s) & 0xffu) << (8 * (i % 4));
+  }
+  return q.finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
+}
+
+// One block of NT threads per sorted row: codes[p] and scales[p] of row p of `in` (through the row map if there is one).
+// HELD: the row's values stay in registers between its maximum and its codes (up to HELD * 8 * NT of them); longer rows are
+// read twice.
+template <class T, int NT, int HELD>
+__global__ __launch_bounds__(NT) void quantize_rows_kernel(I8Ctx c, const T* __restrict__ in, int K, int8_t* __restrict__ codes,
+                                                           float* __restrict__ scales) {
+  __shared__ uint32_t wave_max[NT / 64];
+  const int p = blockIdx.x, tid = threadIdx.x;
+  if (p >= c.offsets[c.n_experts]) return;  // a caller may only know how many rows there are at most
+  if (!c.all_active) {                      // some experts only: the others' rows are left to their own calls
+    const int e = i8_expert_of(c.offsets, c.n_experts, p);
+    if (!c.active.test(e) || c.slot_of[e] < 0) return;
+  }
+  const T* row = in + (size_t)mapped_row(c.row_map, c.map_div, p) * K;
+  float v[HELD][8];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int k = 8 * (i * NT + tid);
+    if (k < K) {
+      load_8(row + k, v[i]);
+      m = max(m, magnitude_bits(v[i]));
+    }
+  }
+  for (int k = 8 * (HELD * NT + tid); k < K; k += 8 * NT) {
+    float far[8];
+    load_8(row + k, far);
+    m = max(m, magnitude_bits(far));
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
+  if (NT > 64) {
+    if (tid % 64 == 0) wave_max[tid / 64] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) m = max(m, wave_max[w]);
+  }
+  const RowQuant q = row_quant(m);
+  constexpr bool DIVIDE = sizeof(T) == 2;
+  int8_t* out = codes + (size_t)p * K;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int k = 8 * (i * NT + tid);
+    if (k < K) *(uint2*)(out + k) = codes_of<DIVIDE>(v[i], q);
+  }
+  for (int k = 8 * (HELD * NT + tid); k < K; k += 8 * NT) {
+    float far[8];
+    load_8(row + k, far);
+    *(uint2*)(out + k) = codes_of<DIVIDE>(far, q);
+  }
+  if (tid == 0) scales[p] = q.scale;
+}
+
+template <class T>
+static void launch_quantize(const I8Ctx& c, int n_rows, const T* in, int K, int8_t* codes, float* scales, hipStream_t s) {
+  auto launch = [&](auto kernel, int nt) { hipLaunchKernelGGL(kernel, dim3((unsigned)n_rows), dim3(nt), 0, s, c, in, K, codes, scales); };
+  if (K <= 512) launch(&quantize_rows_kernel<T, 64, 1>, 64);
+  else if (K <= 2048) launch(&quantize_rows_kernel<T, 256, 1>, 256);
+  else if (K <= 4096) launch(&quantize_rows_kernel<T, 256, 2>, 256);
+  else launch(&quantize_rows_kernel<T, 1024, 2>, 1024);
+}
+
+// ---- the reference path: one wavefront per output element ------------------------------------
+__device__ __forceinline__ int dot_16(const int4& a, const int4& b, int acc) {
+  acc = __builtin_amdgcn_sdot4(a.x, b.x, acc, false);
+  acc = __builtin_amdgcn_sdot4(a.y, b.y, acc, false);
+  acc = __builtin_amdgcn_sdot4(a.z, b.z, acc, false);
+  return __builtin_amdgcn_sdot4(a.w, b.w, acc, false);
+}
+__device__ __forceinline__ int wave_sum_int(int v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+__device__ __forceinline__ const char* i8_row_slot(const I8Ctx& c, int p) {
+  if (p >= c.offsets[c.n_experts]) return nullptr;
+  const int e = i8_expert_of(c.offsets, c.n_experts, p);
+  const int s = c.slot_of[e];
+  return c.active.test(e) && s >= 0 ? c.slots + (size_t)s * c.slot_bytes : nullptr;
+}
+
+__global__ __launch_bounds__(256) void ref_gateup_i8(I8Ctx c, const int8_t* __restrict__ x, const float* __restrict__ x_scales,
+                                                     float* __restrict__ h) {
+  const int p = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int f = blockIdx.y * 4 + wave;
+  const char* slot = i8_row_slot(c, p);
+  if (!slot || f >= c.ffn) return;
+  const I8Offsets off = i8_offsets((size_t)c.hidden, (size_t)c.ffn);
+  const int n_gate = 2 * TILE_N * (f / TILE_N) + f % TILE_N, n_up = n_gate + TILE_N;
+  const int8_t* xr = x + (size_t)p * c.hidden;
+  int g = 0, u = 0;
+  for (int k = 16 * lane; k < c.hidden; k += 16 * 64) {
+    const int4 xv = *(const int4*)(xr + k);
+    g = dot_16(*(const int4*)(slot + i8_packed_index(n_gate, k, c.hidden)), xv, g);
+    u = dot_16(*(const int4*)(slot + i8_packed_index(n_up, k, c.hidden)), xv, u);
+  }
+  g = wave_sum_int(g);
+  u = wave_sum_int(u);
+  if (lane == 0) {
+    const float sx = x_scales[p];
+    const float gf = (float)g * (sx * ((const float*)(slot + off.gate_scales))[f]);
+    const float uf = (float)u * (sx * ((const float*)(slot + off.up_scales))[f]);
+    h[(size_t)p * c.ffn + f] = gf / (1.0f + expf(-gf)) * uf;
+  }
+}
+
+__global__ __launch_bounds__(256) void ref_down_i8(I8Ctx c, const int8_t* __restrict__ h, const float* __restrict__ h_scales,
+                                                   bf16_t* __restrict__ o) {
+  const int p = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int n = blockIdx.y * 4 + wave;
+  const char* slot = i8_row_slot(c, p);
+  if (!slot || n >= c.hidden) return;
+  const I8Offsets off = i8_offsets((size_t)c.hidden, (size_t)c.ffn);
+  const int8_t* hr = h + (size_t)p * c.ffn;
+  int acc = 0;
+  for (int k = 16 * lane; k < c.ffn; k += 16 * 64)
+    acc = dot_16(*(const int4*)(slot + off.down + i8_packed_index(n, k, c.ffn)), *(const int4*)(hr + k), acc);
+  acc = wave_sum_int(acc);
+  if (lane == 0)
+    o[(size_t)p * c.hidden + n] = f32_to_bf16_any((float)acc * (h_scales[p] * ((const float*)(slot + off.down_scales))[n]));
+}
+
+int launch_ffn_reference_i8(const FfnArgs& a) {
+  const hmoe_layer_desc& d = *a.desc;
+  if (a.n_rows == 0) return HMOE_OK;
+  I8Ctx c{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, a.all_active, d.n_experts, d.hidden, d.ffn, a.row_map, a.map_div};
+  const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
+  float* h = (float*)a.h;
+  int8_t* codes = (int8_t*)a.h + w.codes;
+  float* scales = (float*)((char*)a.h + w.scales);
+  launch_quantize(c, a.n_rows, (const bf16_t*)a.x_perm, d.hidden, codes, scales, a.stream);
+  c.row_map = nullptr;  // everything behind it is in sorted order
+  probe_before(a.stream);
+  hipLaunchKernelGGL(ref_gateup_i8, dim3((unsigned)a.n_rows, (unsigned)((d.ffn + 3) / 4)), dim3(256), 0, a.stream, c, codes, scales, h);
+  probe_after(a.stream);
+  launch_quantize(c, a.n_rows, (const float*)h, d.ffn, codes, scales, a.stream);
+  probe_before(a.stream);
+  hipLaunchKernelGGL(ref_down_i8, dim3((unsigned)a.n_rows, (unsigned)((d.hidden + 3) / 4)), dim3(256), 0, a.stream, c, codes, scales,
+                     (bf16_t*)a.o_perm);
+  probe_after(a.stream);
+  HMOE_HIP(hipGetLastError());
+  return HMOE_OK;
+}
+
+}  // namespace hmoe

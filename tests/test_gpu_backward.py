@@ -1,0 +1,246 @@
+"""The layer's gradients around its experts on the GPU against the oracle in 64 bits.
+
+Tolerances: a product or sum of n terms in fp32, in whatever order, is off by at most n 2^-24 times the sum of the terms'
+magnitudes (and one step more for each term's own rounding); a result in bfloat16 by 2^-8 of its value besides."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import workloads as wl
+from oracle import grad_oracle as go
+from hmoe_testlib import to_device, to_host_f32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def hm():
+    import paper_2504_05897_amd as hm
+    return hm
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+class Problem:
+    def __init__(self, hm, dtype, T, H, E, K, seed=0, scale=1.0):
+        rng = np.random.default_rng(seed)
+        self.bf16 = dtype != "f32"
+        kind = {"f32": hm.HMOE_F32, "bf16": hm.HMOE_BF16, "w4": hm.HMOE_BF16_W4, "i8": hm.HMOE_BF16_I8}[dtype]
+        self.desc = hm.make_desc(H, 128, E, K, E, kind)
+        self.dt = torch.bfloat16 if self.bf16 else torch.float32
+        self.step = 2.0 ** -8 if self.bf16 else U
+        A = T * K
+        store = lambda *s: wl.store((rng.standard_normal(s) * scale).astype(np.float32), wl.BF16 if self.bf16 else wl.F32)
+        self.dy, self.o, self.dx_perm, self.x, self.w_g, self.add = (store(*s) for s in ((T, H), (A, H), (A, H), (T, H), (E, H), (T, H)))
+        self.idx = np.argsort(rng.standard_normal((T, E)), axis=1)[:, :K].astype(np.int32)
+        w = np.exp(rng.standard_normal((T, K)))
+        self.w = (w / w.sum(1, keepdims=True)).astype(np.float32)
+        self.dw = rng.standard_normal((T, K)).astype(np.float32)
+        self.inv = np.empty(A, np.int32)
+        self.inv[np.argsort(self.idx.ravel(), kind="stable")] = np.arange(A)
+        self.d_logits = rng.standard_normal((T, E)).astype(np.float32)
+
+    def empty(self, *shape, dtype=None):
+        return torch.full(shape, float("nan"), dtype=self.dt if dtype is None else dtype, device=DEV)
+
+    def value(self, a):
+        return wl.as_f64(a)
+
+
+SIZES = [("bf16", 1, 8, 1, 1), ("bf16", 1, 2048, 64, 6), ("bf16", 3, 136, 5, 3), ("bf16", 70, 1032, 40, 8), ("bf16", 33, 4104, 9, 2),
+         ("bf16", 9, 512, 32, 12), ("f32", 1, 1, 2, 1), ("f32", 7, 37, 8, 2), ("f32", 16, 256, 8, 2), ("f32", 130, 520, 20, 9),
+         ("w4", 5, 128, 4, 2), ("i8", 5, 128, 4, 2)]
+
+
+@pytest.mark.parametrize("dtype,T,H,E,K", SIZES)
+def test_combine_backward(hm, dtype, T, H, E, K):
+    say("combine backward", dtype, T, H, E, K)
+    p = Problem(hm, dtype, T, H, E, K)
+    A = T * K
+    d_o, d_w = p.empty(A, H), p.empty(T, K, dtype=torch.float32)
+    dy, o, inv, w = (to_device(a) for a in (p.dy, p.o, p.inv, p.w))
+    hm.hmoe_combine_backward(p.desc, dy, o, inv, w, T, d_o, d_w)
+    torch.cuda.synchronize()
+    ref_o, ref_w = go.combine_backward(p.value(p.dy), p.value(p.o), p.inv, p.w)
+    assert (np.abs(to_host_f32(d_o) - ref_o) <= p.step * np.abs(ref_o) + 2 * U * np.abs(ref_o)).all()
+    mags = np.stack([(np.abs(p.value(p.dy)[t]) * np.abs(p.value(p.o)[p.inv[t * K:(t + 1) * K]])).sum(1) for t in range(T)])
+    assert (np.abs(to_host_f32(d_w) - ref_w) <= (H + 1) * U * mags).all()
+    # one result at a time, and the rows' gradient in the place of the rows: the same bits
+    alone_o, alone_w = p.empty(A, H), p.empty(T, K, dtype=torch.float32)
+    hm.hmoe_combine_backward(p.desc, dy, None, inv, w, T, alone_o, None)
+    hm.hmoe_combine_backward(p.desc, dy, o, inv, None, T, None, alone_w)
+    again = p.empty(T, K, dtype=torch.float32)
+    hm.hmoe_combine_backward(p.desc, dy, o, inv, w, T, o, again)
+    torch.cuda.synchronize()
+    for a, b in ((alone_o, d_o), (alone_w, d_w), (o, d_o), (again, d_w)):
+        assert torch.equal(a, b)
+
+
+def test_combine_backward_of_assignments_without_a_row(hm):
+    say("combine backward, rows missing")
+    p = Problem(hm, "bf16", 6, 64, 4, 2)
+    inv = p.inv.copy()
+    lost = [inv[3], inv[8]]
+    inv[3], inv[8] = -1, 12
+    d_o, d_w = torch.full((12, 64), 7.0, dtype=torch.bfloat16, device=DEV), p.empty(6, 2, dtype=torch.float32)
+    hm.hmoe_combine_backward(p.desc, to_device(p.dy), to_device(p.o), to_device(inv), to_device(p.w), 6, d_o, d_w)
+    torch.cuda.synchronize()
+    ref_o, ref_w = go.combine_backward(p.value(p.dy), p.value(p.o), inv, p.w)
+    got_o, got_w = to_host_f32(d_o), to_host_f32(d_w)
+    assert got_w.ravel()[3] == 0 and got_w.ravel()[8] == 0 and (got_o[lost] == 7.0).all()
+    keep = np.setdiff1d(np.arange(12), lost)
+    assert (np.abs(got_o[keep] - ref_o[keep]) <= (2.0 ** -8 + 2 * U) * np.abs(ref_o[keep])).all()
+    assert np.allclose(got_w, ref_w, atol=1e-3)
+
+
+@pytest.mark.parametrize("dtype,T,H,E,K", SIZES)
+def test_permute_backward(hm, dtype, T, H, E, K):
+    say("permute backward", dtype, T, H, E, K)
+    p = Problem(hm, dtype, T, H, E, K, seed=1)
+    d, inv, add = to_device(p.dx_perm), to_device(p.inv), to_device(p.add)
+    mags = np.abs(p.value(p.dx_perm))[p.inv].reshape(T, K, H).sum(1)
+    for extra in (None, add):
+        dx = p.empty(T, H)
+        hm.hmoe_permute_backward(p.desc, d, inv, T, extra, dx)
+        torch.cuda.synchronize()
+        ref = go.permute_backward(p.value(p.dx_perm), p.inv, T, None if extra is None else p.value(p.add))
+        slack = (K + 1) * U * (mags + (0 if extra is None else np.abs(p.value(p.add))))
+        assert (np.abs(to_host_f32(dx) - ref) <= p.step * (np.abs(ref) + slack) + slack).all()
+    hm.hmoe_permute_backward(p.desc, d, inv, T, add, add)      # in the place of what is added
+    torch.cuda.synchronize()
+    assert torch.equal(add, dx)
+
+
+@pytest.mark.parametrize("T,E,K", [(1, 1, 1), (5, 8, 2), (300, 9, 9), (77, 16, 3), (2, 31, 31), (64, 64, 6), (9, 100, 8), (33, 256, 32)])
+def test_route_backward(hm, T, E, K):
+    say("route backward", T, E, K)
+    p = Problem(hm, "bf16", T, 8, E, K, seed=2)
+    d = p.empty(T, E, dtype=torch.float32)
+    hm.hmoe_route_backward(p.desc, to_device(p.idx), to_device(p.w), to_device(p.dw), T, d)
+    torch.cuda.synchronize()
+    ref = go.route_backward(p.idx, p.w, p.dw, E)
+    largest = np.abs(p.dw).max(1, keepdims=True)               # |dw - mean| <= 2 largest; the mean is a sum of K terms
+    assert (np.abs(d.cpu().numpy() - ref) <= 2 * (K + 3) * U * largest * (ref != 0)).all()
+
+
+def test_route_backward_of_odd_choices(hm):
+    """An id that a token names twice gets the sum of both; ids outside the experts are left out."""
+    say("route backward, odd ids")
+    desc = hm.make_desc(8, 128, 5, 3, 5, hm.HMOE_BF16)
+    idx = np.array([[1, 1, 4], [0, -1, 2], [5, 3, 3]], np.int32)
+    rng = np.random.default_rng(0)
+    w, dw = rng.random((3, 3)).astype(np.float32), rng.standard_normal((3, 3)).astype(np.float32)
+    d = torch.full((3, 5), float("nan"), device=DEV)
+    hm.hmoe_route_backward(desc, to_device(idx), to_device(w), to_device(dw), 3, d)
+    torch.cuda.synchronize()
+    assert np.allclose(d.cpu().numpy(), go.route_backward(idx, w, dw, 5), atol=1e-6)
+
+
+ROUTER = [("bf16", 1, 16, 1, 1), ("bf16", 1, 2048, 64, 6), ("bf16", 17, 144, 5, 3), ("bf16", 200, 1040, 40, 8), ("bf16", 33, 4112, 9, 2),
+          ("bf16", 513, 512, 97, 12), ("bf16", 66, 48, 256, 8), ("bf16", 1500, 272, 64, 2), ("f32", 1, 1, 2, 1), ("f32", 7, 37, 8, 2),
+          ("f32", 16, 256, 8, 2), ("f32", 700, 130, 67, 9), ("f32", 2100, 36, 33, 2), ("i8", 40, 128, 4, 2)]
+
+
+@pytest.mark.parametrize("dtype,T,H,E,K", ROUTER)
+def test_router_backward(hm, dtype, T, H, E, K):
+    say("router backward", dtype, T, H, E, K)
+    p = Problem(hm, dtype, T, H, E, K, seed=3)
+    x, w_g, d, add = (to_device(a) for a in (p.x, p.w_g, p.d_logits, p.add))
+    n = hm.hmoe_router_backward_workspace_bytes(p.desc, T)
+    ws = torch.full((n + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    xv, wv, dv = p.value(p.x), p.value(p.w_g), p.d_logits.astype(np.float64)
+    dx_mags, dw_mags = np.abs(dv) @ np.abs(wv), np.abs(dv).T @ np.abs(xv)
+    results = []
+    for extra in (None, add):
+        dx, d_w = p.empty(T, H), p.empty(E, H, dtype=torch.float32)
+        hm.hmoe_router_backward(p.desc, x, w_g, d, T, extra, dx, d_w, ws, n)
+        torch.cuda.synchronize()
+        ref_dx, ref_dw = go.router_backward(xv, wv, dv, None if extra is None else p.value(p.add))
+        slack = (E + 2) * U * (dx_mags + (0 if extra is None else np.abs(p.value(p.add))))
+        if p.bf16:
+            # the kernel may carry d_logits in two pieces of 8 bits: 2^-17 of each term
+            slack = slack + 2.0 ** -17 * dx_mags
+        assert (np.abs(to_host_f32(dx) - ref_dx) <= p.step * (np.abs(ref_dx) + slack) + slack).all()
+        assert (np.abs(to_host_f32(d_w) - ref_dw) <= (T + 2) * U * dw_mags).all()
+        results.append((dx, d_w))
+    assert (ws[n:] == 0x5a).all()
+    dx, d_w = results[1]
+    only_dx, only_dw = p.empty(T, H), p.empty(E, H, dtype=torch.float32)
+    hm.hmoe_router_backward(p.desc, None, w_g, d, T, add, only_dx, None, ws, n)
+    hm.hmoe_router_backward(p.desc, x, None, d, T, None, None, only_dw, ws, n)
+    hm.hmoe_router_backward(p.desc, x, w_g, d, T, add, add, None, ws, n)       # in the place of what is added
+    torch.cuda.synchronize()
+    assert torch.equal(only_dx, dx) and torch.equal(only_dw, d_w) and torch.equal(add, dx)
+
+
+def test_router_backward_of_no_tokens_writes_zeros(hm):
+    say("router backward, no tokens")
+    desc = hm.make_desc(64, 128, 5, 2, 5, hm.HMOE_BF16)
+    n = hm.hmoe_router_backward_workspace_bytes(desc, 0)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    d_w = torch.full((5, 64), 7.0, device=DEV)
+    hm.hmoe_router_backward(desc, None, None, None, 0, None, None, d_w, ws, n)
+    torch.cuda.synchronize()
+    assert (d_w == 0).all()
+
+
+@pytest.mark.parametrize("where", ["x", "d_logits"])
+def test_router_backward_carries_infinities_and_nans(hm, where):
+    """A value that is not finite reaches the results it takes part in, and no others."""
+    say("router backward, not finite", where)
+    p = Problem(hm, "bf16", 40, 64, 6, 2, seed=5)
+    x, d = p.x.copy(), p.d_logits.copy()
+    if where == "x":
+        x[7, 3] = 0x7fc0
+    else:
+        d[7, 2] = np.inf
+    n = hm.hmoe_router_backward_workspace_bytes(p.desc, 40)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    dx, d_w = p.empty(40, 64), p.empty(6, 64, dtype=torch.float32)
+    hm.hmoe_router_backward(p.desc, to_device(x), to_device(p.w_g), to_device(d), 40, None, dx, d_w, ws, n)
+    torch.cuda.synchronize()
+    dx, d_w = ~np.isfinite(to_host_f32(dx)), ~np.isfinite(to_host_f32(d_w))
+    if where == "x":
+        assert not dx.any() and d_w[:, 3].all() and not np.delete(d_w, 3, 1).any()
+    else:
+        assert dx[7].all() and not np.delete(dx, 7, 0).any() and d_w[2].all() and not np.delete(d_w, 2, 0).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_in_a_graph(hm, dtype):
+    """All four captured together and replayed on new inputs, with eager work in between: the eager results' bits."""
+    say("gradients in a graph", dtype)
+    T, H, E, K = 600, 256, 24, 4
+    p = Problem(hm, dtype, T, H, E, K, seed=6)
+    dy, o, inv, w, idx, x, w_g, dxp = (to_device(a) for a in (p.dy, p.o, p.inv, p.w, p.idx, p.x, p.w_g, p.dx_perm))
+    n = hm.hmoe_router_backward_workspace_bytes(p.desc, T)
+
+    def chain(ws):
+        d_o, d_w, dx = p.empty(T * K, H), p.empty(T, K, dtype=torch.float32), p.empty(T, H)
+        d_l, d_wg = p.empty(T, E, dtype=torch.float32), p.empty(E, H, dtype=torch.float32)
+        hm.hmoe_combine_backward(p.desc, dy, o, inv, w, T, d_o, d_w)
+        hm.hmoe_permute_backward(p.desc, dxp, inv, T, None, dx)
+        hm.hmoe_route_backward(p.desc, idx, w, d_w, T, d_l)
+        hm.hmoe_router_backward(p.desc, x, w_g, d_l, T, dx, dx, d_wg, ws, n)
+        return [d_o, d_w, dx, d_l, d_wg]
+
+    ws = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    chain(ws[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = chain(ws[0])
+    for seed in range(3):
+        dy.copy_(to_device(Problem(hm, dtype, T, H, E, K, seed=30 + seed).dy))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = chain(ws[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed

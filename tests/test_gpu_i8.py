@@ -1,0 +1,301 @@
+"""Experts in 8-bit integers (HMOE_BF16_I8) on the GPU against the oracle's evaluation in 64 bits.
+
+Tolerance: an output is off by at most the slack that the oracle states for an evaluation in fp32 (codes of h that lie within
+2^-10 of a half may be the other whole number) and half a step of bfloat16, 2^-8 of the value."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import workloads as wl
+from oracle import i8_oracle as i8
+from hmoe_testlib import to_device, to_host_f32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SKINNY, TILED, REFERENCE = 2, 3, 1
+
+
+@pytest.fixture(scope="module")
+def hm():
+    import paper_2504_05897_amd as hm
+    return hm
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def offsets_of(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+def check_rows(o, x, offsets, experts):
+    """o [A, H] against the oracle, expert by expert"""
+    o = to_host_f32(o) if isinstance(o, torch.Tensor) else o
+    for e, (lo, hi) in enumerate(zip(offsets[:-1], offsets[1:])):
+        if hi > lo:
+            ref, slack = i8.expert_ffn(wl.as_f64(x[lo:hi]), *(wl.as_f64(m) for m in experts[e]))
+            err = np.abs(o[lo:hi] - ref)
+            bound = slack + 2.0 ** -8 * (np.abs(ref) + slack)
+            assert (err <= bound).all(), (e, float((err - bound).max()), float(np.abs(ref).max()))
+            assert np.abs(ref).max() > 1e-3
+
+
+def make(hm, hidden, ffn, n_experts, top_k, seed, distinct=None, max_tokens=1):
+    """A layer whose experts repeat `distinct` different ones."""
+    distinct = n_experts if distinct is None else distinct
+    shape = wl.small_shape(dtype=wl.BF16, hidden=hidden, ffn=ffn, n_experts=distinct, top_k=1)
+    some = wl.make_layer(shape, seed, n_tokens=1).experts
+    experts = [some[e % distinct] for e in range(n_experts)]
+    d = hm.make_desc(hidden, ffn, n_experts, top_k, n_experts, hm.HMOE_BF16_I8)
+    return d, experts, hm.MoELayer(d, experts, (), None, max_tokens=max_tokens, host_copies=False)
+
+
+def rows_of(seed, n, hidden):
+    return wl.store(np.random.default_rng(seed).standard_normal((n, hidden)).astype(np.float32), wl.BF16)
+
+
+def workspace(hm, d, A):
+    """exactly what the call asks for, with a margin behind it that has to stay as it is"""
+    n = hm.hmoe_ffn_workspace_bytes(d, A)
+    ws = torch.full((n + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    return ws, n
+
+
+def grouped(hm, d, layer, x, offsets, A, path, active=None, o=None, stream=None):
+    ws, n = workspace(hm, d, A)
+    o = torch.full((A, d.hidden), float("nan"), dtype=torch.bfloat16, device=DEV) if o is None else o
+    hm.hmoe_expert_ffn_grouped(d, layer.cache, x, offsets, A, active, o, ws, n, path, stream)
+    torch.cuda.synchronize()
+    assert (ws[n:] == 0x5a).all()
+    return o
+
+
+@pytest.mark.parametrize("path", [REFERENCE, SKINNY, TILED])
+@pytest.mark.parametrize("hidden,ffn,counts", [
+    (128, 128, [1]),                              # one row, one K unit in both products
+    (256, 128, [3, 0, 7, 1, 40, 0, 9, 2]),        # decode-sized groups and one of several passes
+    (128, 384, [33, 1, 0, 0, 70, 5, 8, 32]),      # an odd number of K units; a half-filled column tile
+    (1024, 256, [0, 0, 0, 1, 0, 0, 0, 0]),
+    (2176, 640, [16, 17, 31]),                    # 17 and 5 K units
+    (640, 512, [130, 0, 64, 257]),                # several row tiles with ragged ends
+    (256, 4352, [2, 9]),                          # rows of h longer than a block of the quantiser holds at once
+])
+def test_ffn_i8_paths(hm, path, hidden, ffn, counts):
+    say("ffn i8", path, hidden, ffn, counts)
+    d, experts, layer = make(hm, hidden, ffn, len(counts), 1, hidden + ffn, distinct=min(3, len(counts)))
+    offsets = offsets_of(counts)
+    A = int(offsets[-1])
+    x = rows_of(5, A, hidden)
+    o = grouped(hm, d, layer, to_device(x), to_device(offsets), A, path)
+    check_rows(o, x, offsets, experts)
+    layer.close()
+
+
+def test_paths_agree_bit_for_bit(hm):
+    """The sums are exact: the decode and the prefill kernels leave the same bits."""
+    say("i8 paths agree")
+    counts = [1, 0, 5, 32, 30]
+    d, experts, layer = make(hm, 768, 896, len(counts), 1, 3)
+    offsets = to_device(offsets_of(counts))
+    x = to_device(rows_of(2, sum(counts), 768))
+    a, b = (grouped(hm, d, layer, x, offsets, sum(counts), p) for p in (SKINNY, TILED))
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    layer.close()
+
+
+@pytest.mark.parametrize("path", [REFERENCE, SKINNY, TILED])
+def test_rows_with_special_values(hm, path):
+    """Zeros give zeros; an infinity or a NaN makes its own row NaN and no other; the largest and smallest values count."""
+    say("i8 special rows", path)
+    d, experts, layer = make(hm, 256, 128, 2, 1, 7)
+    x = wl.as_f32(rows_of(1, 40, 256)).copy()
+    x[0] = 0
+    x[1, 7] = np.inf
+    x[2, 255] = -np.inf
+    x[3, 0] = np.nan
+    x[4] = 0
+    x[4, 9] = 1.0                                   # one value in the row
+    x[5] *= np.float32(2.0 ** -110)                 # below the smallest amax
+    x[6] = np.where(np.arange(256) % 2, 1e-3, 1e-3)  # all alike: every code 127
+    bits = wl.store(x, wl.BF16)
+    o = to_host_f32(grouped(hm, d, layer, to_device(bits), to_device(offsets_of([20, 20])), 40, path))
+    assert (o[0] == 0).all() and np.isnan(o[1:4]).all()
+    keep = np.array([i for i in range(40) if not 1 <= i <= 3])
+    assert np.isfinite(o[keep]).all()
+    for e, rows in ((0, keep[keep < 20]), (1, keep[keep >= 20])):
+        ref, slack = i8.expert_ffn(wl.as_f64(bits[rows]), *(wl.as_f64(m) for m in experts[e]))
+        # (2^-100: a result that small may be a denormal or zero)
+        assert (np.abs(o[rows] - ref) <= slack + 2.0 ** -8 * (np.abs(ref) + slack) + 2.0 ** -100).all()
+    layer.close()
+
+
+@pytest.mark.parametrize("path", [REFERENCE, SKINNY, TILED])
+def test_huge_values_do_not_overflow_in_the_quantiser(hm, path):
+    """Values near the end of bfloat16's range: 127 v would be infinite.  Weights small enough that h is finite."""
+    say("i8 huge", path)
+    d = hm.make_desc(128, 128, 1, 1, 1, hm.HMOE_BF16_I8)
+    rng = np.random.default_rng(0)
+    w = [wl.store((rng.standard_normal((128, 128)) * s).astype(np.float32), wl.BF16) for s in (2.0 ** -126, 2.0 ** -126, 1.0)]
+    layer = hm.MoELayer(d, [tuple(w)], (), None, max_tokens=1, host_copies=False)
+    x = wl.store((rng.standard_normal((3, 128)) * 6e37).astype(np.float32), wl.BF16)
+    o = grouped(hm, d, layer, to_device(x), to_device(offsets_of([3])), 3, path)
+    # the gate and up weights lie below 2^-100: their codes are those of amax = 2^-100, as the oracle's are
+    check = to_host_f32(o)
+    ref, slack = i8.expert_ffn(wl.as_f64(x), *(wl.as_f64(m) for m in w))
+    assert np.isfinite(check).all() and (np.abs(check - ref) <= slack + 2.0 ** -8 * (np.abs(ref) + slack) + 2.0 ** -100).all()
+    layer.close()
+
+
+@pytest.mark.parametrize("path", [REFERENCE, SKINNY, TILED])
+def test_only_rows_of_active_and_resident_experts_are_written(hm, path):
+    say("i8 active", path)
+    counts = [4, 9, 0, 40, 2]
+    d, experts, layer = make(hm, 256, 256, len(counts), 1, 9)
+    offsets = offsets_of(counts)
+    A = int(offsets[-1])
+    n_rows = A + 37                                  # a caller may only know how many rows there are at most
+    x = rows_of(3, A, 256)
+    hm.hmoe_cache_evict(layer.cache, 1)
+    o = torch.full((A, 256), 7.0, dtype=torch.bfloat16, device=DEV)
+    grouped(hm, d, layer, to_device(x), to_device(offsets), n_rows, path, active=[0, 3], o=o)
+    got = to_host_f32(o)
+    for e, (lo, hi) in enumerate(zip(offsets[:-1], offsets[1:])):
+        if e in (0, 3):
+            ref, slack = i8.expert_ffn(wl.as_f64(x[lo:hi]), *(wl.as_f64(m) for m in experts[e]))
+            assert (np.abs(got[lo:hi] - ref) <= slack + 2.0 ** -8 * (np.abs(ref) + slack)).all()
+        else:
+            assert (got[lo:hi] == 7.0).all()
+    o.fill_(7.0)                                     # every resident expert, one is not
+    grouped(hm, d, layer, to_device(x), to_device(offsets), n_rows, path, o=o)
+    got = to_host_f32(o)
+    assert (got[4:13] == 7.0).all() and (got[:4] != 7.0).any() and (got[13:] != 7.0).any()
+    with pytest.raises(hm.HmoeError) as ei:
+        grouped(hm, d, layer, to_device(x), to_device(offsets), n_rows, path, active=[1], o=o)
+    assert ei.value.status == hm.HMOE_ERR_NOT_RESIDENT
+    layer.close()
+
+
+@pytest.mark.parametrize("path", [0, REFERENCE, SKINNY, TILED])
+def test_gather_of_some_assignments(hm, path):
+    """The rows a permutation names need not be the first A / K of x.  The same bits as over the gathered rows."""
+    say("i8 gather", path)
+    d, experts, layer = make(hm, 256, 128, 4, 2, 3, max_tokens=9)
+    x = to_device(rows_of(4, 9, 256))
+    perm = torch.tensor([17, 3, 12, 5, 16], dtype=torch.int32, device=DEV)
+    offsets = torch.tensor([0, 2, 2, 4, 5], dtype=torch.int32, device=DEV)
+    ws, n = workspace(hm, d, 5)
+    a, b = (torch.full((5, 256), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    hm.hmoe_expert_ffn_grouped_gather(d, layer.cache, x, perm, offsets, 5, None, a, ws, n, path)
+    hm.hmoe_expert_ffn_grouped(d, layer.cache, x[(perm // 2).long()].contiguous(), offsets, 5, None, b, ws, n, path)
+    torch.cuda.synchronize()
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and a.isfinite().all()
+    layer.close()
+
+
+def check_layer(layer, lay, y, T):
+    idx, w = layer.topk_idx[:T].cpu().numpy(), layer.topk_w[:T].cpu().numpy()
+    f64 = lambda experts: [tuple(wl.as_f64(m) for m in e) for e in experts]
+    ref, bound = i8.moe_layer(wl.as_f64(lay.x[:T]), idx, w, f64(lay.experts), f64(lay.shared))
+    assert (np.abs(to_host_f32(y) - ref) <= bound).all()
+
+
+@pytest.mark.parametrize("T", [1, 5, 40, 200])
+@pytest.mark.parametrize("n_slots", [5, 8])
+def test_i8_layer_with_shared_experts(hm, T, n_slots):
+    """Whole forward passes: router, routing, FFN (staged where the cache is partial), shared experts, weighted sum."""
+    say("i8 layer", T, n_slots)
+    shape = wl.small_shape(dtype=wl.BF16, hidden=256, ffn=128, n_experts=8, top_k=2, n_slots=n_slots, shared_ffn=(128, 128),
+                           x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 40 + T, T)
+    d = hm.make_desc(256, 128, 8, 2, n_slots, hm.HMOE_BF16_I8)
+    layer = hm.MoELayer(d, lay.experts, lay.shared, lay.w_router, max_tokens=T)
+    y = layer.forward(to_device(lay.x))
+    torch.cuda.synchronize()
+    check_layer(layer, lay, y, T)
+    plain = y.clone()
+    layer.fused = layer.overlap_shared = layer.merge_shared = False      # the separate calls, the same bits
+    assert torch.equal(layer.forward(to_device(lay.x)).view(torch.int16), plain.view(torch.int16))
+    layer.close()
+
+
+def test_i8_expert_ffn_combine_is_the_calls_it_stands_for(hm):
+    say("i8 merged combine")
+    shape = wl.small_shape(dtype=wl.BF16, hidden=256, ffn=128, n_experts=8, top_k=2, n_slots=8, shared_ffn=(128,), x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 4, 3)
+    d = hm.make_desc(256, 128, 8, 2, 8, hm.HMOE_BF16_I8)
+    layer = hm.MoELayer(d, lay.experts, lay.shared, lay.w_router, max_tokens=3)
+    y = layer.forward(to_device(lay.x)).clone()
+    bounds = layer._shared_bounds.data_ptr() + 8 * 3
+    layer.y.zero_()
+    hm.hmoe_expert_ffn_combine(d, layer.cache, to_device(lay.x), layer.perm, layer.inv_perm, layer.topk_w, layer.offsets, 3, layer.o_perm,
+                               layer.ffn_ws, layer.ffn_ws_bytes, layer.shared_desc, layer.shared_cache, bounds, layer.o_shared,
+                               layer.shared_ws, layer.shared_ws_bytes, layer.y, layer.sync, layer.sync_bytes)
+    torch.cuda.synchronize()
+    assert torch.equal(layer.y[:3].view(torch.int16), y.view(torch.int16))
+    layer.close()
+
+
+@pytest.mark.parametrize("T", [1, 6, 70])
+def test_i8_layer_in_a_graph_and_on_other_streams(hm, T):
+    """Captured once, replayed on new inputs with eager calls of another layer in between; and on a stream of its own."""
+    say("i8 graph", T)
+    shape = wl.small_shape(dtype=wl.BF16, hidden=384, ffn=256, n_experts=6, top_k=2, x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 1, T)
+    d = hm.make_desc(384, 256, 6, 2, 6, hm.HMOE_BF16_I8)
+    layer, other = (hm.MoELayer(d, lay.experts, (), lay.w_router, max_tokens=T) for _ in range(2))
+    x = to_device(lay.x)
+    layer.forward(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = layer.forward(x)
+    side = torch.cuda.Stream()
+    for seed in range(4):
+        x.copy_(to_device(rows_of(20 + seed, T, 384)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            want = other.forward(x)
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16)), seed
+    layer.close()
+    other.close()
+
+
+@pytest.mark.parametrize("T", [1, 8])
+def test_mixtral_i8_full_size(hm, T):
+    """Large experts as a decode loop uses them: the wide matrices' weight stream, rows of 14336 values of h."""
+    say("mixtral i8", T)
+    shape = wl.SHAPES["mixtral"]
+    lay = wl.make_layer(shape, 1, T, threads=16)
+    d = hm.make_desc(shape.hidden, shape.ffn, shape.n_experts, shape.top_k, shape.n_experts, hm.HMOE_BF16_I8)
+    layer = hm.MoELayer(d, lay.experts, (), lay.w_router, max_tokens=T, host_copies=False)
+    y = layer.forward(to_device(lay.x))
+    torch.cuda.synchronize()
+    idx, w = layer.topk_idx[:T].cpu().numpy(), layer.topk_w[:T].cpu().numpy()
+    named = sorted(set(idx[:1].ravel()))                       # the first token's experts: the oracle takes a while
+    ref, bound = i8.moe_layer(wl.as_f64(lay.x[:1]), np.searchsorted(named, idx[:1]), w[:1],
+                              [tuple(wl.as_f64(m) for m in lay.experts[e]) for e in named])
+    assert (np.abs(to_host_f32(y[:1]) - ref) <= bound).all()
+    layer.close()
+
+
+def test_a_prefill_batch_of_many_tiles(hm):
+    """More rows per expert than any tile has, skewed: the first expert takes half of them."""
+    say("i8 many tiles")
+    counts = [1100, 0, 300, 513, 1, 77, 128, 31]
+    d, experts, layer = make(hm, 768, 384, len(counts), 1, 11, distinct=2)
+    offsets = offsets_of(counts)
+    A = int(offsets[-1])
+    x = rows_of(6, A, 768)
+    o = grouped(hm, d, layer, to_device(x), to_device(offsets), A, 0)
+    check_rows(o, x, offsets, experts)
+    again = grouped(hm, d, layer, to_device(x), to_device(offsets), A, 0)
+    assert torch.equal(o.view(torch.int16), again.view(torch.int16))
+    layer.close()
