@@ -22,6 +22,13 @@ __device__ __forceinline__ f32x16_t mfma_32x32x16_bf16(u32x4 a, u32x4 b, f32x16_
                                                  0, 0, 0);
 }
 
+// The same in 8-bit integers, K = 32: lane l supplies A[l%32][16*(l/32) .. +16] and B[16*(l/32) .. +16][l%32]; 32-bit sums.
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x16_t __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ i32x16_t mfma_32x32x32_i8(u32x4 a, u32x4 b, i32x16_t c) {
+  return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
+}
+
 // D = A(16x32) * B(32x16) + C.  Lane l supplies A[l%16][8*(l/16) .. +8] and B[8*(l/16) .. +8][l%16];
 // accumulator register r of lane l is D[4*(l/16) + r][l%16].
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -58,6 +65,11 @@ __device__ __forceinline__ int mapped_row(const int32_t* __restrict__ row_map, i
 // silu(g) = g / (1 + exp(-g)) with the hardware reciprocal (1 ulp) in place of an IEEE division: the result is
 // rounded to bf16 right away, and the division costs ten vector instructions per element in the epilogues.
 __device__ __forceinline__ float silu_f32(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+
+// A product of two rows of 8-bit codes from their integer sum and scales (one order of roundings wherever it is taken).
+__device__ __forceinline__ float i8_product(int sum, float row_scale, float col_scale) {
+  return (float)sum * (row_scale * col_scale);
+}
 
 // Experts taking part in one FFN call, one bit per expert id.
 struct ActiveMask {
@@ -221,6 +233,11 @@ int launch_ffn_tiled(const FfnArgs& a);
 int launch_ffn_skinny_w4(const FfnArgs& a);
 int launch_ffn_tiled_w4(const FfnArgs& a);
 int launch_ffn_reference_i8(const FfnArgs& a);
+int launch_ffn_skinny_i8(const FfnArgs& a);
+int launch_ffn_tiled_i8(const FfnArgs& a);
+// codes and scales of the rows that an int8 FFN launch reads, in the call's workspace: the tokens' (sorted), then those of h
+void launch_quantize_x_i8(const FfnArgs& a);
+void launch_quantize_h_i8(const FfnArgs& a);
 
 }  // namespace hmoe
 

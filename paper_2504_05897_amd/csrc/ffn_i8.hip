@@ -180,8 +180,8 @@ __global__ __launch_bounds__(256) void ref_gateup_i8(I8Ctx c, const int8_t* __re
   u = wave_sum_int(u);
   if (lane == 0) {
     const float sx = x_scales[p];
-    const float gf = (float)g * (sx * ((const float*)(slot + off.gate_scales))[f]);
-    const float uf = (float)u * (sx * ((const float*)(slot + off.up_scales))[f]);
+    const float gf = i8_product(g, sx, ((const float*)(slot + off.gate_scales))[f]);
+    const float uf = i8_product(u, sx, ((const float*)(slot + off.up_scales))[f]);
     h[(size_t)p * c.ffn + f] = gf / (1.0f + expf(-gf)) * uf;
   }
 }
@@ -199,23 +199,39 @@ __global__ __launch_bounds__(256) void ref_down_i8(I8Ctx c, const int8_t* __rest
     acc = dot_16(*(const int4*)(slot + off.down + i8_packed_index(n, k, c.ffn)), *(const int4*)(hr + k), acc);
   acc = wave_sum_int(acc);
   if (lane == 0)
-    o[(size_t)p * c.hidden + n] = f32_to_bf16_any((float)acc * (h_scales[p] * ((const float*)(slot + off.down_scales))[n]));
+    o[(size_t)p * c.hidden + n] = f32_to_bf16_any(i8_product(acc, h_scales[p], ((const float*)(slot + off.down_scales))[n]));
+}
+
+static I8Ctx i8_ctx(const FfnArgs& a) {
+  return I8Ctx{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, a.all_active, a.desc->n_experts, a.desc->hidden, a.desc->ffn,
+               a.row_map, a.map_div};
+}
+void launch_quantize_x_i8(const FfnArgs& a) {
+  const I8Work w = i8_work((size_t)a.n_rows, (size_t)a.desc->hidden, (size_t)a.desc->ffn);
+  launch_quantize(i8_ctx(a), a.n_rows, (const bf16_t*)a.x_perm, a.desc->hidden, (int8_t*)a.h + w.codes, (float*)((char*)a.h + w.scales),
+                  a.stream);
+}
+void launch_quantize_h_i8(const FfnArgs& a) {
+  const I8Work w = i8_work((size_t)a.n_rows, (size_t)a.desc->hidden, (size_t)a.desc->ffn);
+  I8Ctx c = i8_ctx(a);
+  c.row_map = nullptr;  // h is in sorted order
+  launch_quantize(c, a.n_rows, (const float*)a.h, a.desc->ffn, (int8_t*)a.h + w.codes, (float*)((char*)a.h + w.scales), a.stream);
 }
 
 int launch_ffn_reference_i8(const FfnArgs& a) {
   const hmoe_layer_desc& d = *a.desc;
   if (a.n_rows == 0) return HMOE_OK;
-  I8Ctx c{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, a.all_active, d.n_experts, d.hidden, d.ffn, a.row_map, a.map_div};
+  if ((d.ffn + 3) / 4 > 65535 || (d.hidden + 3) / 4 > 65535) return HMOE_ERR_UNSUPPORTED;
+  const I8Ctx c = i8_ctx(a);
   const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
-  float* h = (float*)a.h;
-  int8_t* codes = (int8_t*)a.h + w.codes;
-  float* scales = (float*)((char*)a.h + w.scales);
-  launch_quantize(c, a.n_rows, (const bf16_t*)a.x_perm, d.hidden, codes, scales, a.stream);
-  c.row_map = nullptr;  // everything behind it is in sorted order
+  const int8_t* codes = (const int8_t*)a.h + w.codes;
+  const float* scales = (const float*)((const char*)a.h + w.scales);
+  launch_quantize_x_i8(a);
   probe_before(a.stream);
-  hipLaunchKernelGGL(ref_gateup_i8, dim3((unsigned)a.n_rows, (unsigned)((d.ffn + 3) / 4)), dim3(256), 0, a.stream, c, codes, scales, h);
+  hipLaunchKernelGGL(ref_gateup_i8, dim3((unsigned)a.n_rows, (unsigned)((d.ffn + 3) / 4)), dim3(256), 0, a.stream, c, codes, scales,
+                     (float*)a.h);
   probe_after(a.stream);
-  launch_quantize(c, a.n_rows, (const float*)h, d.ffn, codes, scales, a.stream);
+  launch_quantize_h_i8(a);
   probe_before(a.stream);
   hipLaunchKernelGGL(ref_down_i8, dim3((unsigned)a.n_rows, (unsigned)((d.hidden + 3) / 4)), dim3(256), 0, a.stream, c, codes, scales,
                      (bf16_t*)a.o_perm);
