@@ -557,7 +557,7 @@ static int32_t ffn_prepare(const hmoe_layer_desc* desc, hmoe_cache* cache, const
 
 static int32_t ffn_launch(const FfnArgs& a, int32_t path) {
   if (a.desc->dtype == HMOE_BF16_I8)
-    return path == HMOE_FFN_REFERENCE ? launch_ffn_reference_i8(a) : path == HMOE_FFN_SKINNY ? launch_ffn_reference_i8(a) : launch_ffn_tiled_i8(a);
+    return path == HMOE_FFN_REFERENCE ? launch_ffn_reference_i8(a) : path == HMOE_FFN_SKINNY ? launch_ffn_skinny_i8(a) : launch_ffn_tiled_i8(a);
   if (path == FFN_F32_TILES) return launch_ffn_f32(a);
   if (path == HMOE_FFN_REFERENCE) return launch_ffn_reference(a);
   if (path == HMOE_FFN_SKINNY) return a.desc->dtype == HMOE_BF16_W4 ? launch_ffn_skinny_w4(a) : launch_ffn_skinny(a);

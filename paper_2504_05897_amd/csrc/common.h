@@ -28,6 +28,11 @@ typedef int32_t i32x16_t __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ i32x16_t mfma_32x32x32_i8(u32x4 a, u32x4 b, i32x16_t c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
 }
+// D = A(16x64) * B(64x16) + C: lane l supplies A[l%16][16*(l/16) .. +16] and B[16*(l/16) .. +16][l%16]; register r of lane l is
+// D[4*(l/16) + r][l%16].
+__device__ __forceinline__ i32x4_t mfma_16x16x64_i8(u32x4 a, u32x4 b, i32x4_t c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
+}
 
 // D = A(16x32) * B(32x16) + C.  Lane l supplies A[l%16][8*(l/16) .. +8] and B[8*(l/16) .. +8][l%16];
 // accumulator register r of lane l is D[4*(l/16) + r][l%16].

@@ -5,7 +5,7 @@
 // made: the scale of a row is known when its last value is.  It stays in fp32 until then, since a code is decided by where
 // 127 h / amax lies between two halves: 16 bits for it would move one code in a thousand, which is as large an error of the
 // result as its final rounding.
-#include "common.h"
+#include "i8_rows.h"
 
 namespace hmoe {
 
@@ -29,55 +29,6 @@ __device__ __forceinline__ int i8_expert_of(const int32_t* __restrict__ offsets,
     if (offsets[mid] <= p) lo = mid; else hi = mid;
   }
   return lo;
-}
-
-// 8 consecutive values of a row as fp32
-__device__ __forceinline__ void load_8(const bf16_t* p, float (&v)[8]) {
-  const u32x4 u = *(const u32x4*)p;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(u[i] << 16);
-    v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load_8(const float* p, float (&v)[8]) {
-  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ uint32_t magnitude_bits(const float (&v)[8]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  return m;
-}
-// What a row's codes are computed with.  bfloat16 rows: 127 v (exact; scaled by a power of two where it could overflow)
-// divided by amax, one rounding, so that halves are seen as such.  fp32 rows, whose values fall on halves by accident only:
-// times the reciprocal, ten instructions fewer per value.
-struct RowQuant {
-  float times, by, scale;
-  bool finite;
-};
-__device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
-  RowQuant q;
-  q.finite = amax_bits < 0x7f800000u;
-  const float amax = q.finite ? fmaxf(__uint_as_float(amax_bits), I8_MIN_AMAX) : 1.0f;
-  const float down = amax > 0x1p100f ? 0x1p-10f : 1.0f;
-  q.times = 127.0f * down;
-  q.by = amax * down;
-  q.scale = q.finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
-  return q;
-}
-template <bool DIVIDE>
-__device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q) {
-  uint32_t w[2] = {0, 0};
-  const float r = DIVIDE ? 0.0f : q.times / q.by;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float s = DIVIDE ? v[i] * q.times / q.by : v[i] * r;
-    w[i / 4] |= ((uint32_t)__float2int_rn(s) & 0xffu) << (8 * (i % 4));
-  }
-  return q.finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
 }
 
 // One block of NT threads per sorted row: codes[p] and scales[p] of row p of `in` (through the row map if there is one).

@@ -1,0 +1,58 @@
+// Quantisation of rows to 8-bit integers on the device (HMOE_BF16_I8): what the quantising launches and the decode kernel,
+// which quantises a few rows itself, share.
+#pragma once
+
+#include "common.h"
+
+namespace hmoe {
+
+// 8 consecutive values of a row as fp32
+__device__ __forceinline__ void load_8(const bf16_t* p, float (&v)[8]) {
+  const u32x4 u = *(const u32x4*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(u[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load_8(const float* p, float (&v)[8]) {
+  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ uint32_t magnitude_bits(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+// What a row's codes are computed with.  bfloat16 rows: 127 v (exact; scaled by a power of two where it could overflow)
+// divided by amax, one rounding, so that halves are seen as such.  fp32 rows, whose values fall on halves by accident only:
+// times the reciprocal, ten instructions fewer per value.
+struct RowQuant {
+  float times, by, scale;
+  bool finite;
+};
+__device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
+  RowQuant q;
+  q.finite = amax_bits < 0x7f800000u;
+  const float amax = q.finite ? fmaxf(__uint_as_float(amax_bits), I8_MIN_AMAX) : 1.0f;
+  const float down = amax > 0x1p100f ? 0x1p-10f : 1.0f;
+  q.times = 127.0f * down;
+  q.by = amax * down;
+  q.scale = q.finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
+  return q;
+}
+template <bool DIVIDE>
+__device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q) {
+  uint32_t w[2] = {0, 0};
+  const float r = DIVIDE ? 0.0f : q.times / q.by;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = DIVIDE ? v[i] * q.times / q.by : v[i] * r;
+    w[i / 4] |= ((uint32_t)__float2int_rn(s) & 0xffu) << (8 * (i % 4));
+  }
+  return q.finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
+}
+
+}  // namespace hmoe
