@@ -72,28 +72,336 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const int32_t* __re
   }
 }
 
-// dx[t] = sum_e d_logits[t, e] w_g[e] (+ add[t]): one thread per element
-template <class T>
-__global__ __launch_bounds__(256) void router_dx_kernel(const T* __restrict__ w_g, const float* __restrict__ d_logits, const T* add,
-                                                        int n_experts, int hidden, T* dx) {
-  const size_t t = blockIdx.x;
-  const int c = blockIdx.y * 256 + threadIdx.x;
-  if (c >= hidden) return;
-  float acc = 0.0f;
-  for (int e = 0; e < n_experts; ++e) acc = fmaf(d_logits[t * n_experts + e], to_f32(w_g[(size_t)e * hidden + c]), acc);
-  if (add) acc += to_f32(add[t * hidden + c]);
-  from_f32(dx[t * hidden + c], acc);
+// ---- the router's product --------------------------------------------------------------------
+// dx = d_logits . W_g (sum over experts) and d_w_g = d_logits^T . x (sum over tokens), both on matrix instructions whose
+// summed index is the slow one of W_g and x in memory.  No operand is transposed through LDS: lane l of a wave loads 16 bytes,
+// a piece of consecutive columns 16 / sizeof(T) * (l % 16) .., of each of the rows that its k block needs, and column i of every
+// lane's piece makes an operand of its own, for the columns {16 / sizeof(T) * n + i}.  A lane's results are then consecutive
+// columns again.
+//   bfloat16 layers: 16x16x32 instructions; d_logits, fp32, goes in as a sum of bfloat16 pieces, each what is left of the value
+//     cut to its upper 8 bits.  Three pieces hold all 24 bits of a value; dx, which is rounded to bfloat16, takes two
+//     (the second rounded: 2^-17 of a term).  The fp32 instruction would take 27 us for each product of 16384 x 64 x 2048.
+//   fp32 layers: 16x16x4 fp32 instructions.
+
+// N of 16-bit pairs: operand dwords (rows 2 d, 2 d + 1) of the lower / upper halves of one dword column of eight rows
+__device__ __forceinline__ void transpose_halves(const uint32_t (&rows)[8], u32x4& lower, u32x4& upper) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    lower[d] = __builtin_amdgcn_perm(rows[2 * d + 1], rows[2 * d], 0x05040100u);
+    upper[d] = __builtin_amdgcn_perm(rows[2 * d + 1], rows[2 * d], 0x07060302u);
+  }
+}
+// the next piece of eight values: their upper halves as an operand, which are taken out of the values
+__device__ __forceinline__ u32x4 take_piece(float (&v)[8]) {
+  u32x4 piece;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    piece[d] = __builtin_amdgcn_perm(__float_as_uint(v[2 * d + 1]), __float_as_uint(v[2 * d]), 0x07060302u);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+  return piece;
+}
+__device__ __forceinline__ u32x4 round_piece(const float (&v)[8]) {
+  return u32x4{f32_to_bf16_pair(v[0], v[1]), f32_to_bf16_pair(v[2], v[3]), f32_to_bf16_pair(v[4], v[5]), f32_to_bf16_pair(v[6], v[7])};
+}
+// values i0 .. i0 + 4 of a row of n (0 past its end); whole: rows and their pieces are 16-byte aligned
+__device__ __forceinline__ f32x4_t load_4(const float* row, int i0, int n, bool whole) {
+  if (whole) return i0 < n ? *(const f32x4_t*)(row + i0) : f32x4_t{0, 0, 0, 0};
+  f32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = i0 + i < n ? row[i0 + i] : 0.0f;
+  return v;
+}
+__device__ __forceinline__ f32x4_t mfma_16x16x4_f32(float a, float b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// d_w_g[e] = sum_t d_logits[t, e] x[t]: one thread per element
-template <class T>
-__global__ __launch_bounds__(256) void router_dw_kernel(const T* __restrict__ x, const float* __restrict__ d_logits, int n_tokens,
-                                                        int n_experts, int hidden, float* __restrict__ d_w_g) {
-  const int e = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= hidden) return;
-  float acc = 0.0f;
-  for (int t = 0; t < n_tokens; ++t) acc = fmaf(d_logits[(size_t)t * n_experts + e], to_f32(x[(size_t)t * hidden + c]), acc);
-  d_w_g[(size_t)e * hidden + c] = acc;
+constexpr int RB_WAVES = 4;
+constexpr int DX_COLS_BF16 = 128, DX_COLS_F32 = 64;  // columns of a wave: 16 pieces of 16 bytes
+
+// dx, bfloat16: a wave takes 16 RF tokens x 128 columns and goes through the experts 32 at a time.
+template <int RF>
+__global__ __launch_bounds__(64 * RB_WAVES) void router_dx_bf16_kernel(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits,
+                                                                       const bf16_t* add, int n_tokens, int n_experts, int hidden, bf16_t* dx) {
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int t0 = (blockIdx.x * RB_WAVES + wave) * 16 * RF;
+  const int col = blockIdx.y * DX_COLS_BF16 + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
+  if (t0 >= n_tokens) return;
+  const bool whole = n_experts % 4 == 0;
+  f32x4_t acc[RF][8];
+#pragma unroll
+  for (int f = 0; f < RF; ++f)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[f][i] = f32x4_t{0, 0, 0, 0};
+  for (int e0 = 0; e0 < n_experts; e0 += 32) {
+    const int e = e0 + 8 * kblk;
+    u32x4 w[8], op[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = *(const u32x4*)(w_g + (size_t)min(e + k, n_experts - 1) * hidden + col_at);
+    f32x4_t d[RF][2];
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+      const float* row = d_logits + (size_t)min(t0 + 16 * f + n, n_tokens - 1) * n_experts;
+      d[f][0] = load_4(row, e, n_experts, whole);
+      d[f][1] = load_4(row, e + 4, n_experts, whole);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)  // (a row of W_g past the last would meet zeros, but may hold an infinity)
+      if (e + k >= n_experts) w[k] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t rows[8] = {w[0][p], w[1][p], w[2][p], w[3][p], w[4][p], w[5][p], w[6][p], w[7][p]};
+      transpose_halves(rows, op[2 * p], op[2 * p + 1]);
+    }
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+      float v[8] = {d[f][0][0], d[f][0][1], d[f][0][2], d[f][0][3], d[f][1][0], d[f][1][1], d[f][1][2], d[f][1][3]};
+      const u32x4 hi = take_piece(v), lo = round_piece(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[f][i] = mfma_16x16x32_bf16(hi, op[i], acc[f][i]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[f][i] = mfma_16x16x32_bf16(lo, op[i], acc[f][i]);
+    }
+  }
+  // register r of lane (n, kblk) is token 4 kblk + r of its fragment, operand i column 8 n + i
+  if (col >= hidden) return;
+#pragma unroll
+  for (int f = 0; f < RF; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = t0 + 16 * f + 4 * kblk + r;
+      if (t >= n_tokens) continue;
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = acc[f][i][r];
+      if (add) {
+        const u32x4 s = *(const u32x4*)(add + (size_t)t * hidden + col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[2 * i] += __uint_as_float(s[i] << 16);
+          v[2 * i + 1] += __uint_as_float(s[i] & 0xffff0000u);
+        }
+      }
+      *(u32x4*)(dx + (size_t)t * hidden + col) = round_piece(v);
+    }
+}
+
+// dx, fp32: a wave takes 16 RF tokens x 64 columns and goes through the experts 16 at a time; instruction s of a step has
+// experts 4 (l / 16) + s.
+template <int RF>
+__global__ __launch_bounds__(64 * RB_WAVES) void router_dx_f32_kernel(const float* __restrict__ w_g, const float* __restrict__ d_logits,
+                                                                      const float* add, int n_tokens, int n_experts, int hidden, float* dx) {
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int t0 = (blockIdx.x * RB_WAVES + wave) * 16 * RF;
+  const int col = blockIdx.y * DX_COLS_F32 + 4 * n;
+  if (t0 >= n_tokens) return;
+  const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
+  f32x4_t acc[RF][4];
+#pragma unroll
+  for (int f = 0; f < RF; ++f)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[f][i] = f32x4_t{0, 0, 0, 0};
+  for (int e0 = 0; e0 < n_experts; e0 += 16) {
+    const int e = e0 + 4 * kblk;
+    f32x4_t w[4], d[RF];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      w[s] = e + s < n_experts ? load_4(w_g + (size_t)(e + s) * hidden, col, hidden, whole_h) : f32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int f = 0; f < RF; ++f) d[f] = load_4(d_logits + (size_t)min(t0 + 16 * f + n, n_tokens - 1) * n_experts, e, n_experts, whole_e);
+#pragma unroll
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[f][i] = mfma_16x16x4_f32(d[f][s], w[s][i], acc[f][i]);
+  }
+#pragma unroll
+  for (int f = 0; f < RF; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = t0 + 16 * f + 4 * kblk + r;
+      if (t >= n_tokens) continue;
+      f32x4_t v = {acc[f][0][r], acc[f][1][r], acc[f][2][r], acc[f][3][r]};
+      if (add) v += load_4(add + (size_t)t * hidden, col, hidden, whole_h);
+      float* out = dx + (size_t)t * hidden;
+      if (whole_h && col < hidden) *(f32x4_t*)(out + col) = v;
+      else
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (col + i < hidden) out[col + i] = v[i];
+    }
+}
+
+// d_w_g: a block takes 64 experts x DwShape::COLS columns over one chunk of the tokens, each of its waves every fourth step of
+// STEP tokens; the waves' sums meet in LDS, the chunks' in router_dw_sum_kernel, all in a fixed order.
+struct DwBf16 {
+  typedef bf16_t T;
+  static constexpr int COLS = 128, STEP = 32, PIECE = 8;
+};
+struct DwF32 {
+  typedef float T;
+  static constexpr int COLS = 64, STEP = 16, PIECE = 4;
+};
+constexpr int DW_EXPERTS = 64;
+
+// the operands of a step: tokens t .. + 8 of the lane's k block
+struct DwStepBf16 {
+  u32x4 x[8];
+  f32x4_t d[8];
+  __device__ __forceinline__ void load(const bf16_t* __restrict__ x_in, const float* __restrict__ d_logits, int t0, int t_end, int col_at,
+                                       int e, int n_experts, int hidden, bool whole_e, bool, int kblk) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int t = t0 + 8 * kblk + k, at = min(t, t_end - 1);
+      x[k] = *(const u32x4*)(x_in + (size_t)at * hidden + col_at);
+      d[k] = load_4(d_logits + (size_t)at * n_experts, e, n_experts, whole_e);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)  // (both: zero times an infinity is none)
+      if (t0 + 8 * kblk + k >= t_end) {
+        x[k] = u32x4{0, 0, 0, 0};
+        d[k] = f32x4_t{0, 0, 0, 0};
+      }
+  }
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[4][8]) const {
+    u32x4 op[8];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t rows[8] = {x[0][p], x[1][p], x[2][p], x[3][p], x[4][p], x[5][p], x[6][p], x[7][p]};
+      transpose_halves(rows, op[2 * p], op[2 * p + 1]);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      float v[8] = {d[0][m], d[1][m], d[2][m], d[3][m], d[4][m], d[5][m], d[6][m], d[7][m]};
+#pragma unroll
+      for (int piece = 0; piece < 3; ++piece) {
+        const u32x4 a = take_piece(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[m][i] = mfma_16x16x32_bf16(a, op[i], acc[m][i]);
+      }
+    }
+  }
+};
+struct DwStepF32 {
+  f32x4_t x[4], d[4];
+  __device__ __forceinline__ void load(const float* __restrict__ x_in, const float* __restrict__ d_logits, int t0, int t_end, int col_at, int e,
+                                       int n_experts, int hidden, bool whole_e, bool whole_h, int kblk) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = t0 + 4 * k + kblk;
+      const bool there = t < t_end;
+      x[k] = there ? load_4(x_in + (size_t)t * hidden, col_at, hidden, whole_h) : f32x4_t{0, 0, 0, 0};
+      d[k] = there ? load_4(d_logits + (size_t)t * n_experts, e, n_experts, whole_e) : f32x4_t{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[4][4]) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m][i] = mfma_16x16x4_f32(d[k][m], x[k][i], acc[m][i]);
+  }
+};
+
+template <class SHAPE, class DW_STEP>
+__global__ __launch_bounds__(64 * RB_WAVES) void router_dw_kernel(const typename SHAPE::T* __restrict__ x, const float* __restrict__ d_logits,
+                                                                     int n_tokens, int n_experts, int hidden, int chunk_tokens,
+                                                                     float* __restrict__ out) {
+  constexpr int PIECE = SHAPE::PIECE;
+  __shared__ float red[RB_WAVES][PIECE * 4][64];
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int col = blockIdx.x * SHAPE::COLS + PIECE * n;
+  const int col_at = SHAPE::PIECE == 8 ? min(col, hidden - 8) : col;  // (fp32 rows of any length are checked where they are read)
+  const int t_begin = blockIdx.y * chunk_tokens, t_end = min(t_begin + chunk_tokens, n_tokens);
+  const int e0 = blockIdx.z * DW_EXPERTS, e = e0 + 4 * n;  // operand m of the lane: expert e0 + 4 n + m
+  const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
+  f32x4_t acc[4][PIECE];
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) acc[m][i] = f32x4_t{0, 0, 0, 0};
+  DW_STEP step;
+  int t = t_begin + wave * SHAPE::STEP;
+  if (t < t_end) {
+    step.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
+    for (;;) {
+      const DW_STEP now = step;
+      t += RB_WAVES * SHAPE::STEP;
+      if (t >= t_end) {
+        now.multiply(acc);
+        break;
+      }
+      step.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
+      now.multiply(acc);
+    }
+  }
+  // register r of lane (n, kblk) is row 4 kblk + r of the instruction: expert e0 + 4 (4 kblk + r) + m; operand i column PIECE n + i
+  out += (size_t)blockIdx.y * n_experts * hidden;
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) red[wave][i * 4 + r][lane] = acc[m][i][r];
+    __syncthreads();
+    const int r = wave, to = e0 + 4 * (4 * kblk + r) + m;  // a thread per row and piece of columns
+    static_assert(RB_WAVES == 4, "");
+    float v[PIECE];
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) {
+      v[i] = red[0][i * 4 + r][lane];
+#pragma unroll
+      for (int w = 1; w < RB_WAVES; ++w) v[i] += red[w][i * 4 + r][lane];
+    }
+    if (to < n_experts) {
+      float* row = out + (size_t)to * hidden + col;
+#pragma unroll
+      for (int i = 0; i < PIECE; i += 4) {
+        if (whole_h && col + i < hidden) *(f32x4_t*)(row + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+        else
+#pragma unroll
+          for (int k = i; k < i + 4; ++k)
+            if (col + k < hidden) row[k] = v[k];
+      }
+    }
+  }
+}
+
+// d_w_g = sum of the chunks' parts
+__global__ __launch_bounds__(256) void router_dw_sum_kernel(const float* __restrict__ parts, int n_chunks, long n, float* __restrict__ out) {
+  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  if (n % 4 == 0) {
+    f32x4_t v = *(const f32x4_t*)(parts + i);
+#pragma unroll 8
+    for (int c = 1; c < n_chunks; ++c) v += *(const f32x4_t*)(parts + (long)c * n + i);
+    *(f32x4_t*)(out + i) = v;
+  } else {
+    for (long k = i; k < i + 4 && k < n; ++k) {
+      float v = parts[k];
+      for (int c = 1; c < n_chunks; ++c) v += parts[(long)c * n + k];
+      out[k] = v;
+    }
+  }
+}
+
+// Chunks of the tokens in the d_w_g launch: as many as give every CU a block, of 128 tokens or more.
+struct DwPlan {
+  int columns, expert_tiles, chunks, chunk_tokens;
+};
+static DwPlan dw_plan(const hmoe_layer_desc& d, int T) {
+  DwPlan p;
+  const int cols = d.dtype == HMOE_F32 ? DwF32::COLS : DwBf16::COLS;
+  p.columns = (d.hidden + cols - 1) / cols;
+  p.expert_tiles = (d.n_experts + DW_EXPERTS - 1) / DW_EXPERTS;
+  const long blocks = (long)p.columns * p.expert_tiles;
+  const int want = (int)std::max(1l, std::min(256 / blocks, (long)(T + 127) / 128));
+  p.chunk_tokens = std::max(1, ((T + want - 1) / want + 127) / 128 * 128);
+  p.chunks = std::max(1, (T + p.chunk_tokens - 1) / p.chunk_tokens);
+  return p;
 }
 
 }  // namespace hmoe
@@ -147,7 +455,8 @@ extern "C" int32_t hmoe_route_backward(const hmoe_layer_desc* desc, const int32_
 
 extern "C" size_t hmoe_router_backward_workspace_bytes(const hmoe_layer_desc* desc, int32_t T) {
   if (check_desc(desc) != HMOE_OK || T < 0) return 0;
-  return 256;
+  const DwPlan p = dw_plan(*desc, T);
+  return p.chunks > 1 ? (size_t)p.chunks * desc->n_experts * desc->hidden * sizeof(float) : 16;
 }
 
 extern "C" int32_t hmoe_router_backward(const hmoe_layer_desc* desc, const void* x, const void* w_g, const float* d_logits, int32_t T,
@@ -155,7 +464,7 @@ extern "C" int32_t hmoe_router_backward(const hmoe_layer_desc* desc, const void*
   int rc = check_desc(desc);
   if (rc != HMOE_OK) return rc;
   const int E = desc->n_experts, H = desc->hidden;
-  if (T < 0) return HMOE_ERR_INVALID_ARG;
+  if (T < 0 || T > 0x7fffffff / desc->top_k || T > 0x7fff0000) return HMOE_ERR_INVALID_ARG;  // (token numbers past the last tile fit)
   if (!dx && !d_w_g) return HMOE_ERR_INVALID_ARG;
   if (T > 0 && (!d_logits || (dx && !w_g) || (d_w_g && !x))) return HMOE_ERR_INVALID_ARG;
   if (!aligned16(d_logits) || (dx && (!aligned16(dx) || !aligned16(w_g) || !aligned16(add))) || (d_w_g && (!aligned16(d_w_g) || !aligned16(x))))
@@ -164,20 +473,32 @@ extern "C" int32_t hmoe_router_backward(const hmoe_layer_desc* desc, const void*
   if (!workspace || workspace_bytes < hmoe_router_backward_workspace_bytes(desc, T)) return HMOE_ERR_WORKSPACE;
   if (!aligned16(workspace)) return HMOE_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
-  const unsigned columns = (unsigned)((H + 255) / 256);
+  const bool f32 = desc->dtype == HMOE_F32;
   if (dx && T > 0) {
-    const dim3 grid((unsigned)T, columns);
-    if (desc->dtype == HMOE_F32)
-      hipLaunchKernelGGL(router_dx_kernel<float>, grid, dim3(256), 0, s, (const float*)w_g, d_logits, (const float*)add, E, H, (float*)dx);
-    else
-      hipLaunchKernelGGL(router_dx_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)w_g, d_logits, (const bf16_t*)add, E, H, (bf16_t*)dx);
+    const int columns = f32 ? DX_COLS_F32 : DX_COLS_BF16, slices = (H + columns - 1) / columns;
+    // 64 tokens per wave where that leaves every SIMD one, else 16
+    const int rf = (long)slices * (T / 64) >= 1024 ? 4 : 1;
+    const dim3 grid((unsigned)((T + 16l * rf * RB_WAVES - 1) / (16l * rf * RB_WAVES)), (unsigned)slices);
+    auto launch = [&](auto kernel, auto type) {
+      typedef decltype(type) V;
+      hipLaunchKernelGGL(kernel, grid, dim3(64 * RB_WAVES), 0, s, (const V*)w_g, d_logits, (const V*)add, T, E, H, (V*)dx);
+    };
+    if (f32) launch(rf == 4 ? &router_dx_f32_kernel<4> : &router_dx_f32_kernel<1>, 0.0f);
+    else launch(rf == 4 ? &router_dx_bf16_kernel<4> : &router_dx_bf16_kernel<1>, bf16_t{});
   }
   if (d_w_g) {
-    const dim3 grid(columns, (unsigned)E);
-    if (desc->dtype == HMOE_F32)
-      hipLaunchKernelGGL(router_dw_kernel<float>, grid, dim3(256), 0, s, (const float*)x, d_logits, T, E, H, d_w_g);
+    const DwPlan p = dw_plan(*desc, T);
+    float* out = p.chunks > 1 ? (float*)workspace : d_w_g;
+    const dim3 grid((unsigned)p.columns, (unsigned)p.chunks, (unsigned)p.expert_tiles);
+    if (f32)
+      hipLaunchKernelGGL((router_dw_kernel<DwF32, DwStepF32>), grid, dim3(64 * RB_WAVES), 0, s, (const float*)x, d_logits, T, E, H, p.chunk_tokens, out);
     else
-      hipLaunchKernelGGL(router_dw_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)x, d_logits, T, E, H, d_w_g);
+      hipLaunchKernelGGL((router_dw_kernel<DwBf16, DwStepBf16>), grid, dim3(64 * RB_WAVES), 0, s, (const bf16_t*)x, d_logits, T, E, H,
+                         p.chunk_tokens, out);
+    if (p.chunks > 1) {
+      const long n = (long)E * H;
+      hipLaunchKernelGGL(router_dw_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, (const float*)workspace, p.chunks, n, d_w_g);
+    }
   }
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;

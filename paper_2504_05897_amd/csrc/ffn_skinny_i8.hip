@@ -10,11 +10,9 @@
 //   * K is dealt to the NW waves in steps of 64, round-robin, so that the block sweeps one contiguous stretch; DEPTH steps are
 //     in flight per wave.  Loads go through buffer descriptors: one lane offset, a scalar offset per load; a lane without a
 //     token fetches nothing and gets zeros, which add nothing to integer sums.
-//   * With at most SKINNY_I8_ROWS tokens a block quantises the rows it needs itself, into LDS, while its first codes are on
+//   * In small calls (in_blocks below) a block quantises the rows it needs itself, into LDS, while its first codes are on
 //     their way: two launches instead of four, and the rows' maxima cost each block a trip to the L2 that holds them.
 //   * The waves' sums meet in LDS; they are exact, so neither the split nor its order shows in the result.
-#include <stdlib.h>
-
 #include <algorithm>
 
 #include "i8_rows.h"
@@ -29,6 +27,7 @@ struct SkinnyI8Ctx {
   ActiveMask active;
   int n_experts, hidden, ffn;
   uint32_t in_bytes;       // of the codes of all rows
+  int own_rows;            // rows per pass of a block that quantises them itself, up to SKINNY_I8_ROWS
   const int32_t* row_map;  // rows quantised in the gate/up launch: input row of sorted row p is row_map[p] / map_div
   int map_div;
 };
@@ -96,7 +95,7 @@ __device__ __forceinline__ void own_row_codes(const T* __restrict__ row, int K, 
   if (tid == 0) *scale = q.scale;
 }
 
-constexpr int SKINNY_I8_ROWS = 4;       // rows per pass of a block that quantises them itself
+constexpr int SKINNY_I8_ROWS = 8;       // rows per pass of a block that quantises them itself
 constexpr int SKINNY_I8_ROW_PAD = 16;   // bytes between their codes in LDS
 
 // GATEUP: codes of the tokens [A, H] -> h [A, F] fp32;  else: codes of h [A, F] -> o_perm [A, H] bfloat16.
@@ -106,7 +105,7 @@ template <bool GATEUP, int NW, int XF, int DEPTH, bool OWN>
 __global__ __launch_bounds__(64 * NW) void ffn_skinny_i8_kernel(SkinnyI8Ctx c, const void* __restrict__ in,
                                                                  const float* __restrict__ row_scales, void* __restrict__ out) {
   static_assert(!OWN || XF == 1, "");
-  extern __shared__ __attribute__((aligned(16))) int8_t own_codes[];  // [SKINNY_I8_ROWS][K + pad]
+  extern __shared__ __attribute__((aligned(16))) int8_t own_codes[];  // [own_rows][K + pad]
   __shared__ float own_scales[SKINNY_I8_ROWS];
   __shared__ uint32_t own_max[NW];
   constexpr int NMAT = GATEUP ? 2 : 1;
@@ -133,7 +132,7 @@ __global__ __launch_bounds__(64 * NW) void ffn_skinny_i8_kernel(SkinnyI8Ctx c, c
   const int n_steps = K / 64, per_wave = (n_steps + NW - 1) / NW;  // steps per wave (the last ones may lie past the end)
   constexpr uint32_t NO_ROW = 0xF0000000u;
 
-  constexpr int PASS = OWN ? SKINNY_I8_ROWS : 16 * XF;
+  const int PASS = OWN ? c.own_rows : 16 * XF;
   for (int row0 = row_first; row0 < row_end; row0 += PASS) {
     const int rows = min(PASS, row_end - row0);
     uint32_t xin[XF];
@@ -246,7 +245,7 @@ template <bool GATEUP, int XF, bool OWN>
 static void launch_stage_i8(const SkinnyI8Ctx& c, int busy_max, const void* in, const float* row_scales, void* out, hipStream_t s) {
   const dim3 grid((unsigned)((GATEUP ? c.ffn : c.hidden) / TILE_N), (unsigned)busy_max);
   const int K = GATEUP ? c.hidden : c.ffn, n_steps = K / 64;
-  const size_t lds = OWN ? (size_t)SKINNY_I8_ROWS * (K + SKINNY_I8_ROW_PAD) : 0;
+  const size_t lds = OWN ? (size_t)c.own_rows * (K + SKINNY_I8_ROW_PAD) : 0;
   auto launch = [&](auto kernel, int nw) { hipLaunchKernelGGL(kernel, grid, dim3(64 * nw), lds, s, c, in, row_scales, out); };
   if (n_steps < 48) launch(&ffn_skinny_i8_kernel<GATEUP, 2, XF, 4, OWN>, 2);
   else if (n_steps < 112) launch(&ffn_skinny_i8_kernel<GATEUP, 4, XF, 4, OWN>, 4);
@@ -260,18 +259,23 @@ int launch_ffn_skinny_i8(const FfnArgs& a) {
   // offsets of 32 bits, and a margin in which lanes without a token stay past the end at every step
   const size_t x_bytes = (size_t)a.n_rows * d.hidden, h_bytes = (size_t)a.n_rows * d.ffn;
   if (std::max(x_bytes, h_bytes) > 0xE0000000u) return launch_ffn_tiled_i8(a);
-  SkinnyI8Ctx c{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, d.n_experts, d.hidden, d.ffn, (uint32_t)x_bytes, a.row_map, a.map_div};
+  SkinnyI8Ctx c{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, d.n_experts, d.hidden, d.ffn, (uint32_t)x_bytes, 0, a.row_map, a.map_div};
   const int busy_max = std::min(d.n_experts, a.n_rows);          // every busy expert has at least one row
   const int max_rows = std::max(1, a.n_rows / d.top_k);          // a token names an expert at most once
   const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
   const int8_t* codes = (const int8_t*)a.h + w.codes;
   const float* scales = (const float*)((const char*)a.h + w.scales);
-  int own_rows = SKINNY_I8_ROWS;
-  if (const char* env = getenv("HMOE_I8_OWN")) own_rows = atoi(env);
-  constexpr size_t OWN_LDS = 60 * 1024;  // of codes, at most
-  const bool own_x = max_rows <= own_rows && (size_t)SKINNY_I8_ROWS * (d.hidden + SKINNY_I8_ROW_PAD) <= OWN_LDS;
-  const bool own_h = max_rows <= own_rows && (size_t)SKINNY_I8_ROWS * (d.ffn + SKINNY_I8_ROW_PAD) <= OWN_LDS;
+  // Rows quantised by the blocks that read them (max_rows of them per pass, in LDS) or by a launch of its own.  The launch
+  // costs 3 to 4 us; in a block it costs time per row, and that again in every round of blocks.  Calls, own launches / in the
+  // blocks, us: 64 experts of 2048 x 1408, top 6, 1 / 4 / 8 tokens 19.0 / 16.5, 39.6 / 35.6, 61.0 / 58.7; 16 of 4096 x 1024, top 2, 8 tokens
+  // 32.2 / 27.7; 8 of 4096 x 14336, top 2, 2 tokens (28672 values of h per pass) 115.0 / 112.4, 4 tokens (57344) 143.8 / 146.2, 8 tokens
+  // (3584 blocks in gate/up) 198.4 / 206.2; 64 of 3584 x 2560, top 8, 8 tokens (5120 blocks) 198.1 / 199.4.
+  auto in_blocks = [&](int K, int n_out) {
+    return max_rows <= SKINNY_I8_ROWS && max_rows * K <= 32768 && (long)(n_out / TILE_N) * busy_max <= 3000;
+  };
+  const bool own_x = in_blocks(d.hidden, d.ffn), own_h = in_blocks(d.ffn, d.hidden);
   const bool two = max_rows > 16;
+  c.own_rows = max_rows;
   if (!own_x) launch_quantize_x_i8(a);
   probe_before(a.stream);
   if (own_x) launch_stage_i8<true, 1, true>(c, busy_max, a.x_perm, nullptr, a.h, a.stream);
