@@ -13,32 +13,84 @@ __device__ __forceinline__ float sum_over_wave(float v) {
   return v;
 }
 
-__device__ __forceinline__ float to_f32(bf16_t v) { return bf16_to_f32(v); }
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ void from_f32(bf16_t& o, float v) { o = f32_to_bf16_any(v); }
-__device__ __forceinline__ void from_f32(float& o, float v) { o = v; }
+// Pieces of a row: 16 bytes (VEC of N elements), or one fp32 element where rows are no multiple of that.
+template <class VEC>
+struct Piece;
+template <>
+struct Piece<u32x4> {  // bfloat16
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void dot(float (&sum)[2], const u32x4& a, const u32x4& b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum[0] = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16), sum[0]);
+      sum[1] = fmaf(__uint_as_float(a[i] & 0xffff0000u), __uint_as_float(b[i] & 0xffff0000u), sum[1]);
+    }
+  }
+  static __device__ __forceinline__ u32x4 times(const u32x4& a, float w) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = f32_to_bf16_pair(w * __uint_as_float(a[i] << 16), w * __uint_as_float(a[i] & 0xffff0000u));
+    return r;
+  }
+};
+template <>
+struct Piece<f32x4_t> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void dot(float (&sum)[2], const f32x4_t& a, const f32x4_t& b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i % 2] = fmaf(a[i], b[i], sum[i % 2]);
+  }
+  static __device__ __forceinline__ f32x4_t times(const f32x4_t& a, float w) { return a * w; }
+};
+template <>
+struct Piece<float> {
+  static constexpr int N = 1;
+  static __device__ __forceinline__ void dot(float (&sum)[2], float a, float b) { sum[0] = fmaf(a, b, sum[0]); }
+  static __device__ __forceinline__ float times(float a, float w) { return a * w; }
+};
 
-// d_o_perm[p] = w dy[t], d_topk_w = dy[t] . o_perm[p]: one wavefront per assignment.  d_o_perm may be o_perm: a lane reads
-// its elements before it writes them.
-template <class T>
-__global__ __launch_bounds__(256) void combine_backward_kernel(const T* dy, const T* o_perm, const int32_t* inv_perm, const float* topk_w,
-                                                               int n_assign, int top_k, int hidden, T* d_o_perm, float* d_topk_w) {
+// d_o_perm[p] = w dy[t], d_topk_w = dy[t] . o_perm[p]: one wavefront per assignment, whose neighbours find dy[t] in the caches.
+// Bound by the rows' trips to memory and back; four pieces per lane are on their way at a time.  STREAM: rows that no cache will
+// hold go past them (16384 tokens of 2048, top 6: SEE_BELOW).  d_o_perm may be o_perm: a lane reads its pieces before it writes
+// them.
+template <class VEC, bool ROWS, bool WEIGHTS, bool STREAM>
+__global__ __launch_bounds__(256) void combine_backward_kernel(const VEC* dy, const VEC* o_perm, const int32_t* inv_perm,
+                                                               const float* topk_w, int n_assign, int top_k, int row_vec, VEC* d_o_perm,
+                                                               float* d_topk_w) {
+  constexpr int AHEAD = 4;
   const int a = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
   if (a >= n_assign) return;
   const int p = inv_perm[a];
-  const bool has_row = (unsigned)p < (unsigned)n_assign;
-  float dot = 0.0f;
-  if (has_row) {
-    const T* g = dy + (size_t)(a / top_k) * hidden;
-    const float w = d_o_perm ? topk_w[a] : 0.0f;
-    for (int c = lane; c < hidden; c += 64) {
-      const float v = to_f32(g[c]);
-      if (d_topk_w) dot += v * to_f32(o_perm[(size_t)p * hidden + c]);
-      if (d_o_perm) from_f32(d_o_perm[(size_t)p * hidden + c], w * v);
+  const float w = ROWS ? topk_w[a] : 0.0f;
+  float sum[2] = {0.0f, 0.0f};
+  if ((unsigned)p < (unsigned)n_assign) {
+    const VEC* g_row = dy + (size_t)(a / top_k) * row_vec;
+    const VEC* o_row = WEIGHTS ? o_perm + (size_t)p * row_vec : nullptr;
+    VEC* d_row = ROWS ? d_o_perm + (size_t)p * row_vec : nullptr;
+    for (int c0 = lane; c0 < row_vec; c0 += 64 * AHEAD) {
+      VEC g[AHEAD], o[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int c = c0 + 64 * i;
+        if (c >= row_vec) continue;
+        g[i] = g_row[c];
+        if (WEIGHTS) o[i] = STREAM ? __builtin_nontemporal_load(o_row + c) : o_row[c];
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int c = c0 + 64 * i;
+        if (c >= row_vec) continue;
+        if (WEIGHTS) Piece<VEC>::dot(sum, g[i], o[i]);
+        if (ROWS) {
+          const VEC r = Piece<VEC>::times(g[i], w);
+          if (STREAM) __builtin_nontemporal_store(r, d_row + c);
+          else d_row[c] = r;
+        }
+      }
     }
   }
-  if (!d_topk_w) return;
-  dot = sum_over_wave(dot);
+  if (!WEIGHTS) return;
+  const float dot = sum_over_wave(sum[0] + sum[1]);
   if (lane == 0) d_topk_w[a] = dot;
 }
 
@@ -419,14 +471,19 @@ extern "C" int32_t hmoe_combine_backward(const hmoe_layer_desc* desc, const void
   if (!aligned4(inv_perm) || !aligned4(topk_w) || !aligned4(d_topk_w)) return HMOE_ERR_INVALID_ARG;
   if (desc->dtype != HMOE_F32 && desc->hidden % 8 != 0) return HMOE_ERR_UNSUPPORTED;
   const int n_assign = T * desc->top_k, H = desc->hidden;
-  const dim3 grid((unsigned)(((long)n_assign + 3) / 4));
-  hipStream_t s = (hipStream_t)stream;
-  if (desc->dtype == HMOE_F32)
-    hipLaunchKernelGGL(combine_backward_kernel<float>, grid, dim3(256), 0, s, (const float*)dy, (const float*)o_perm, inv_perm, topk_w, n_assign,
-                       desc->top_k, H, (float*)d_o_perm, d_topk_w);
-  else
-    hipLaunchKernelGGL(combine_backward_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)dy, (const bf16_t*)o_perm, inv_perm, topk_w,
-                       n_assign, desc->top_k, H, (bf16_t*)d_o_perm, d_topk_w);
+  auto launch = [&](auto type) {
+    typedef decltype(type) VEC;
+    const int row_vec = H / Piece<VEC>::N;
+    const bool stream_past = (size_t)n_assign * row_vec * sizeof(VEC) >= (size_t)64 << 20;
+    const auto kernel = d_o_perm && d_topk_w ? (stream_past ? &combine_backward_kernel<VEC, true, true, true> : &combine_backward_kernel<VEC, true, true, false>)
+                        : d_o_perm           ? (stream_past ? &combine_backward_kernel<VEC, true, false, true> : &combine_backward_kernel<VEC, true, false, false>)
+                                             : (stream_past ? &combine_backward_kernel<VEC, false, true, true> : &combine_backward_kernel<VEC, false, true, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(((long)n_assign + 3) / 4)), dim3(256), 0, (hipStream_t)stream, (const VEC*)dy, (const VEC*)o_perm,
+                       inv_perm, topk_w, n_assign, desc->top_k, row_vec, (VEC*)d_o_perm, d_topk_w);
+  };
+  if (desc->dtype != HMOE_F32) launch(u32x4{});
+  else if (H % 4 == 0) launch(f32x4_t{});
+  else launch(0.0f);
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;
 }

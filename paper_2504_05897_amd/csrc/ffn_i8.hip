@@ -69,17 +69,17 @@ __global__ __launch_bounds__(NT) void quantize_rows_kernel(I8Ctx c, const T* __r
     for (int w = 0; w < NT / 64; ++w) m = max(m, wave_max[w]);
   }
   const RowQuant q = row_quant(m);
-  constexpr bool DIVIDE = sizeof(T) == 2;
+  constexpr bool EXACT = sizeof(T) == 2;
   int8_t* out = codes + (size_t)p * K;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     const int k = 8 * (i * NT + tid);
-    if (k < K) *(uint2*)(out + k) = codes_of<DIVIDE>(v[i], q);
+    if (k < K) *(uint2*)(out + k) = codes_of<EXACT>(v[i], q);
   }
   for (int k = 8 * (HELD * NT + tid); k < K; k += 8 * NT) {
     float far[8];
     load_8(row + k, far);
-    *(uint2*)(out + k) = codes_of<DIVIDE>(far, q);
+    *(uint2*)(out + k) = codes_of<EXACT>(far, q);
   }
   if (tid == 0) scales[p] = q.scale;
 }

@@ -81,16 +81,16 @@ __device__ __forceinline__ void own_row_codes(const T* __restrict__ row, int K, 
 #pragma unroll
   for (int w = 0; w < NW; ++w) m = max(m, wave_max[w]);
   const RowQuant q = row_quant(m);
-  constexpr bool DIVIDE = sizeof(T) == 2;
+  constexpr bool EXACT = sizeof(T) == 2;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     const int k = 8 * (i * 64 * NW + tid);
-    if (k < K) *(uint2*)(codes + k) = codes_of<DIVIDE>(v[i], q);
+    if (k < K) *(uint2*)(codes + k) = codes_of<EXACT>(v[i], q);
   }
   for (int k = 8 * (HELD * 64 * NW + tid); k < K; k += 8 * 64 * NW) {
     float far[8];
     load_8(row + k, far);
-    *(uint2*)(codes + k) = codes_of<DIVIDE>(far, q);
+    *(uint2*)(codes + k) = codes_of<EXACT>(far, q);
   }
   if (tid == 0) *scale = q.scale;
 }

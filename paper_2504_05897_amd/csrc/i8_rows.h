@@ -27,10 +27,12 @@ __device__ __forceinline__ uint32_t magnitude_bits(const float (&v)[8]) {
   return m;
 }
 // What a row's codes are computed with.  bfloat16 rows: 127 v (exact; scaled by a power of two where it could overflow)
-// divided by amax, one rounding, so that halves are seen as such.  fp32 rows, whose values fall on halves by accident only:
-// times the reciprocal, ten instructions fewer per value.
+// divided by amax so that halves are seen as such: the product with the reciprocal, corrected by what it leaves of 127 v.  A
+// quotient that fp32 holds exactly, as every half is, comes out exactly (the correction is then a small multiple of its last
+// bit), and one that is no half is at least 2^-17 of its size away from one.  (A division of the compiler's is ten
+// instructions: 201 million values 158 -> 67 us.)  fp32 rows, whose values fall on halves by accident only: the product alone.
 struct RowQuant {
-  float times, by, scale;
+  float times, by, inverse, scale;
   bool finite;
 };
 __device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
@@ -40,16 +42,18 @@ __device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
   const float down = amax > 0x1p100f ? 0x1p-10f : 1.0f;
   q.times = 127.0f * down;
   q.by = amax * down;
+  q.inverse = __builtin_amdgcn_rcpf(q.by);
   q.scale = q.finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
   return q;
 }
-template <bool DIVIDE>
+template <bool EXACT>
 __device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q) {
   uint32_t w[2] = {0, 0};
-  const float r = DIVIDE ? 0.0f : q.times / q.by;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float s = DIVIDE ? v[i] * q.times / q.by : v[i] * r;
+    const float y = v[i] * q.times;
+    float s = y * q.inverse;
+    if (EXACT) s = fmaf(fmaf(-s, q.by, y), q.inverse, s);
     w[i / 4] |= ((uint32_t)__float2int_rn(s) & 0xffu) << (8 * (i % 4));
   }
   return q.finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
