@@ -31,66 +31,69 @@ __device__ __forceinline__ int i8_expert_of(const int32_t* __restrict__ offsets,
   return lo;
 }
 
-// One block of NT threads per sorted row: codes[p] and scales[p] of row p of `in` (through the row map if there is one).
-// HELD: the row's values stay in registers between its maximum and its codes (up to HELD * 8 * NT of them); longer rows are
-// read twice.
-template <class T, int NT, int HELD>
-__global__ __launch_bounds__(NT) void quantize_rows_kernel(I8Ctx c, const T* __restrict__ in, int K, int8_t* __restrict__ codes,
-                                                           float* __restrict__ scales) {
-  __shared__ uint32_t wave_max[NT / 64];
-  const int p = blockIdx.x, tid = threadIdx.x;
-  if (p >= c.offsets[c.n_experts]) return;  // a caller may only know how many rows there are at most
-  if (!c.all_active) {                      // some experts only: the others' rows are left to their own calls
-    const int e = i8_expert_of(c.offsets, c.n_experts, p);
-    if (!c.active.test(e) || c.slot_of[e] < 0) return;
-  }
+// Whether sorted row p takes part in the launch: a caller may only know how many rows there are at most, and a call over some
+// experts leaves the others' rows to their own calls.
+__device__ __forceinline__ bool row_takes_part(const I8Ctx& c, int p) {
+  if (p >= c.offsets[c.n_experts]) return false;
+  if (c.all_active) return true;
+  const int e = i8_expert_of(c.offsets, c.n_experts, p);
+  return c.active.test(e) && c.slot_of[e] >= 0;
+}
+
+// codes[p] and scales[p] of sorted row p of `in` (through the row map if there is one), whose values stay in registers between
+// the row's maximum and its codes.  Rows of up to 64 * 8 * HELD values: a wavefront each, four per block and no barrier.
+template <class T, int HELD>
+__global__ __launch_bounds__(256) void quantize_rows_wave_kernel(I8Ctx c, const T* __restrict__ in, int n_rows, int K,
+                                                                 int8_t* __restrict__ codes, float* __restrict__ scales) {
+  const int p = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), lane = threadIdx.x % 64;
+  if (p >= n_rows || !row_takes_part(c, p)) return;
   const T* row = in + (size_t)mapped_row(c.row_map, c.map_div, p) * K;
   float v[HELD][8];
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
-    const int k = 8 * (i * NT + tid);
-    if (k < K) {
-      load_8(row + k, v[i]);
-      m = max(m, magnitude_bits(v[i]));
-    }
+    const int k = 8 * (i * 64 + lane);
+    if (k < K) load_8(row + k, v[i]);
   }
-  for (int k = 8 * (HELD * NT + tid); k < K; k += 8 * NT) {
-    float far[8];
-    load_8(row + k, far);
-    m = max(m, magnitude_bits(far));
-  }
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (8 * (i * 64 + lane) < K) m = max(m, magnitude_bits(v[i]));
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
-  if (NT > 64) {
-    if (tid % 64 == 0) wave_max[tid / 64] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) m = max(m, wave_max[w]);
-  }
   const RowQuant q = row_quant(m);
   constexpr bool EXACT = sizeof(T) == 2;
   int8_t* out = codes + (size_t)p * K;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
-    const int k = 8 * (i * NT + tid);
+    const int k = 8 * (i * 64 + lane);
     if (k < K) *(uint2*)(out + k) = codes_of<EXACT>(v[i], q);
   }
-  for (int k = 8 * (HELD * NT + tid); k < K; k += 8 * NT) {
-    float far[8];
-    load_8(row + k, far);
-    *(uint2*)(out + k) = codes_of<EXACT>(far, q);
-  }
-  if (tid == 0) scales[p] = q.scale;
+  if (lane == 0) scales[p] = q.scale;
+}
+
+// Longer rows: a block of 1024 threads each.  What is beyond 16 values per thread is read twice.
+template <class T>
+__global__ __launch_bounds__(1024) void quantize_rows_block_kernel(I8Ctx c, const T* __restrict__ in, int K, int8_t* __restrict__ codes,
+                                                                   float* __restrict__ scales) {
+  __shared__ uint32_t wave_max[16];
+  __shared__ float scale;
+  const int p = blockIdx.x;
+  if (!row_takes_part(c, p)) return;
+  own_row_codes<16, 2>(in + (size_t)mapped_row(c.row_map, c.map_div, p) * K, K, codes + (size_t)p * K, &scale, wave_max);
+  if (threadIdx.x == 0) scales[p] = scale;  // (the thread that wrote it)
 }
 
 template <class T>
 static void launch_quantize(const I8Ctx& c, int n_rows, const T* in, int K, int8_t* codes, float* scales, hipStream_t s) {
-  auto launch = [&](auto kernel, int nt) { hipLaunchKernelGGL(kernel, dim3((unsigned)n_rows), dim3(nt), 0, s, c, in, K, codes, scales); };
-  if (K <= 512) launch(&quantize_rows_kernel<T, 64, 1>, 64);
-  else if (K <= 2048) launch(&quantize_rows_kernel<T, 256, 1>, 256);
-  else if (K <= 4096) launch(&quantize_rows_kernel<T, 256, 2>, 256);
-  else launch(&quantize_rows_kernel<T, 1024, 2>, 1024);
+  auto waves = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((n_rows + 3l) / 4)), dim3(256), 0, s, c, in, n_rows, K, codes, scales);
+  };
+  if (K <= 512) waves(&quantize_rows_wave_kernel<T, 1>);
+  else if (K <= 1024) waves(&quantize_rows_wave_kernel<T, 2>);
+  else if (K <= 1536) waves(&quantize_rows_wave_kernel<T, 3>);
+  else if (K <= 2048) waves(&quantize_rows_wave_kernel<T, 4>);
+  else if (K <= 4096) waves(&quantize_rows_wave_kernel<T, 8>);
+  else hipLaunchKernelGGL(quantize_rows_block_kernel<T>, dim3((unsigned)n_rows), dim3(1024), 0, s, c, in, K, codes, scales);
 }
 
 // ---- the reference path: one wavefront per output element ------------------------------------

@@ -53,48 +53,6 @@ __device__ __forceinline__ bool nth_busy_expert_i8(const SkinnyI8Ctx& c, int wan
   return false;
 }
 
-// Codes and scale of one row, by the whole block (64 NW threads).  HELD: pieces of 8 values that a thread keeps between the
-// maximum and the codes; what is beyond them is read again.
-template <int NW, int HELD, class T>
-__device__ __forceinline__ void own_row_codes(const T* __restrict__ row, int K, int8_t* codes, float* scale, uint32_t* wave_max) {
-  const int tid = threadIdx.x;
-  float v[HELD][8];
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < HELD; ++i) {
-    const int k = 8 * (i * 64 * NW + tid);
-    if (k < K) {
-      load_8(row + k, v[i]);
-      m = max(m, magnitude_bits(v[i]));
-    }
-  }
-  for (int k = 8 * (HELD * 64 * NW + tid); k < K; k += 8 * 64 * NW) {
-    float far[8];
-    load_8(row + k, far);
-    m = max(m, magnitude_bits(far));
-  }
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
-  __syncthreads();  // the last row's maxima have been read
-  if (tid % 64 == 0) wave_max[tid / 64] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NW; ++w) m = max(m, wave_max[w]);
-  const RowQuant q = row_quant(m);
-  constexpr bool EXACT = sizeof(T) == 2;
-#pragma unroll
-  for (int i = 0; i < HELD; ++i) {
-    const int k = 8 * (i * 64 * NW + tid);
-    if (k < K) *(uint2*)(codes + k) = codes_of<EXACT>(v[i], q);
-  }
-  for (int k = 8 * (HELD * 64 * NW + tid); k < K; k += 8 * 64 * NW) {
-    float far[8];
-    load_8(row + k, far);
-    *(uint2*)(codes + k) = codes_of<EXACT>(far, q);
-  }
-  if (tid == 0) *scale = q.scale;
-}
-
 constexpr int SKINNY_I8_ROWS = 8;       // rows per pass of a block that quantises them itself
 constexpr int SKINNY_I8_ROW_PAD = 16;   // bytes between their codes in LDS
 

@@ -20,6 +20,7 @@ __device__ __forceinline__ void load_8(const float* p, float (&v)[8]) {
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
+// the bits of the largest magnitude
 __device__ __forceinline__ uint32_t magnitude_bits(const float (&v)[8]) {
   uint32_t m = 0;
 #pragma unroll
@@ -46,17 +47,65 @@ __device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
   q.scale = q.finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
   return q;
 }
+// The code of a value is the low byte of the value + 1.5 * 2^23, which has no bits behind the point (nearest even).
 template <bool EXACT>
 __device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q) {
-  uint32_t w[2] = {0, 0};
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = v[i] * q.times;
-    float s = y * q.inverse;
-    if (EXACT) s = fmaf(fmaf(-s, q.by, y), q.inverse, s);
-    w[i / 4] |= ((uint32_t)__float2int_rn(s) & 0xffu) << (8 * (i % 4));
+  for (int i = 0; i < 8; i += 4) {
+    uint32_t b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float y = v[i + k] * q.times;
+      float s = y * q.inverse;
+      if (EXACT) s = fmaf(fmaf(-s, q.by, y), q.inverse, s);
+      b[k] = __float_as_uint(s + 12582912.0f);
+    }
+    w[i / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
   }
   return q.finite ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
+}
+
+// Codes and scale of one row, by the whole block (64 NW threads).  HELD: pieces of 8 values that a thread keeps between the
+// maximum and the codes; what is beyond them is read again.
+template <int NW, int HELD, class T>
+__device__ __forceinline__ void own_row_codes(const T* __restrict__ row, int K, int8_t* codes, float* scale, uint32_t* wave_max) {
+  const int tid = threadIdx.x;
+  float v[HELD][8];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int k = 8 * (i * 64 * NW + tid);
+    if (k < K) {
+      load_8(row + k, v[i]);
+      m = max(m, magnitude_bits(v[i]));
+    }
+  }
+  for (int k = 8 * (HELD * 64 * NW + tid); k < K; k += 8 * 64 * NW) {
+    float far[8];
+    load_8(row + k, far);
+    m = max(m, magnitude_bits(far));
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
+  __syncthreads();  // the last row's maxima have been read
+  if (tid % 64 == 0) wave_max[tid / 64] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) m = max(m, wave_max[w]);
+  const RowQuant q = row_quant(m);
+  constexpr bool EXACT = sizeof(T) == 2;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int k = 8 * (i * 64 * NW + tid);
+    if (k < K) *(uint2*)(codes + k) = codes_of<EXACT>(v[i], q);
+  }
+  for (int k = 8 * (HELD * 64 * NW + tid); k < K; k += 8 * 64 * NW) {
+    float far[8];
+    load_8(row + k, far);
+    *(uint2*)(codes + k) = codes_of<EXACT>(far, q);
+  }
+  if (tid == 0) *scale = q.scale;
 }
 
 }  // namespace hmoe
