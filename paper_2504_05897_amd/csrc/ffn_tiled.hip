@@ -159,30 +159,6 @@ static void launch_tiles_fit256w(TiledCtx c, int n_rows, const bf16_t* in, bf16_
 // epilogue a staging region of its own; every vector-memory operation of the kernel after the tile table is issued
 // by hand, except the row-map lookups at the start of a tile, where nothing else is in flight.
 //
-// first loads and copies of a block's first tile (fm copies per thread and stage, into stages 0 and 1)
-template <class TILE>
-__device__ __forceinline__ void walk_issue_prologue(const typename TILE::RowSrc& src, uint32_t lds0, int wave, int fm,
-                                                    u32x4 (&ring)[8][2]) {
-#pragma unroll
-  for (int s = 0; s < 8; ++s)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) ring[s][j] = src.b_at(j, (size_t)s * 64);
-#pragma unroll
-  for (int st = 0; st < 2; ++st)
-#pragma unroll
-    for (int op = 0; op < 7; ++op)
-      if (op < fm) TILE::copy_to_stage(src.a_at(op, (size_t)st * 8), lds0, wave, st, op);  // uniform
-}
-// every vector-memory operation of the thread has completed; the operands tie the weight ring to the wait
-__device__ __forceinline__ void walk_wait_ring(u32x4 (&r)[8][2]) {
-  asm volatile("s_waitcnt vmcnt(0)"
-               : "+v"(r[0][0]), "+v"(r[0][1]), "+v"(r[1][0]), "+v"(r[1][1]), "+v"(r[2][0]), "+v"(r[2][1]), "+v"(r[3][0]),
-                 "+v"(r[3][1]), "+v"(r[4][0]), "+v"(r[4][1]), "+v"(r[5][0]), "+v"(r[5][1]), "+v"(r[6][0]), "+v"(r[6][1]),
-                 "+v"(r[7][0]), "+v"(r[7][1])
-               :
-               : "memory");
-}
-
 // One tile of fm == FM fragments.  In: loc, ring, stage and the thread's seven input rows at rows_lds (a slot of its own
 // per thread and copy, in LDS: registers are short over the K loop) describe the tile, whose first loads have landed.
 // Out: the same for the block's next tile (more: whether there is one), its first loads landed as well.

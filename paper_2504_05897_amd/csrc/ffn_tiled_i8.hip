@@ -78,7 +78,170 @@ __global__ __launch_bounds__(64 * NWV) void ffn_tile256_i8_kernel(TiledCtx c, co
   else run_tile_i8<TileI8<GATEUP, 256, NWV, NT, 8, 2, 1>>(c, in, row_scales, out, loc, lds);
 }
 
-enum { I8_FIT = 0, I8_FIT_PLAIN = 1, I8_FIT4 = 2, I8_FIT4_PLAIN = 3, I8_FIT256 = 4, I8_FIT256_PLAIN = 5 };
+// The 224x256 tile in blocks that work through several tiles, one wave per SIMD (see ffn_tile_walk_kernel).  A tile's last
+// two K steps issue the first loads of the block's next tile, which an int8 tile, with half as many K steps, gains more from.
+// The scales of a tile's rows and columns travel to LDS with two copies issued by hand at its start; the waits of its K steps,
+// which are more than any of them leaves in flight, see them through.
+constexpr int WALK_ROWS = 8;  // per thread in LDS: the input rows of its seven copies, and the row whose scale it copies
+template <bool GATEUP, int FM>
+using WalkI8 = StreamTile<GATEUP, 224, 4, 3, false, 8, FM, 2, true, true, StreamI8>;
+
+struct WalkI8Lds {
+  u32x4 ring[WalkI8<true, 7>::LDS_VEC];
+  u32x4 staging[4 * 64 * 8];
+  float row_scales[2][256], col_scales[2][256];  // of the tile at hand and the next
+  int table[TileWalk<4>::TABLE_INTS];
+  int rows[WALK_ROWS * 256];
+};
+
+// the sorted row whose scale this thread copies: row `tid` of the tile
+__device__ __forceinline__ int walk_scale_row(const TiledCtx& c, const TileLoc& loc, int tid) {
+  return loc.row_first + min(loc.m0 + tid, loc.m_rows - 1);
+}
+
+// One tile of fm == FM fragments whose first K step lies in half START of the weight ring.  In: loc, ring and stage describe the
+// tile, whose first loads have landed; w.rows (gate/up) its input rows.  Out: the same for the block's next tile.
+template <bool GATEUP, bool ODD, int START, int FM, class OUT>
+__device__ __forceinline__ void walk_one_tile_i8(const TiledCtx& c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
+                                                 OUT* __restrict__ out, const TileWalk<4>& walk, int xcd, int stride, int wave, int lane,
+                                                 int k_steps, WalkI8Lds& w, uint32_t lds0, TileLoc& loc, int& idx, int& fm, bool& more,
+                                                 int& stage, int& turn, u32x4 (&ring)[8][2]) {
+  typedef WalkI8<GATEUP, FM> TILE;
+  typedef WalkI8<GATEUP, 7> FULL;
+  const TileLoc done = loc;
+  idx += stride;
+  more = walk.at(xcd, idx, loc);  // leaves loc as it is when there is no further tile
+  fm = loc.fm;
+  int lane_rows = lane;  // (opaque copies of the lane id: what is derived from it is recomputed where it is used)
+  asm volatile("" : "+v"(lane_rows));
+  const int tid_rows = wave * 64 + lane_rows;
+  int* const rows_lds = w.rows + tid_rows;
+  int rows[7], rows_next[7], scale_row, scale_row_next = 0;
+  if constexpr (GATEUP) {
+#pragma unroll
+    for (int i = 0; i < 7; ++i) rows[i] = rows_lds[i * 256];
+    scale_row = rows_lds[7 * 256];
+    FULL::fetch_rows(c, loc, loc.m0, wave, lane_rows, rows_next);
+    scale_row_next = walk_scale_row(c, loc, tid_rows);
+    if (c.row_map) scale_row_next = c.row_map[scale_row_next];
+  } else {
+    FULL::fetch_rows(c, done, done.m0, wave, lane_rows, rows);
+    scale_row = walk_scale_row(c, done, tid_rows);
+  }
+  typename TILE::Acc acc;
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = i32x16_t{0};
+  if constexpr (GATEUP) {
+    // The lookups are waited for here, before the first load issued by hand.
+#pragma unroll
+    for (int i = 0; i < 7; ++i) asm volatile("" : "+v"(rows_next[i]));
+    asm volatile("" : "+v"(scale_row_next));
+    FULL::input_rows(c, rows_next);
+    if (c.row_map) scale_row_next = div_by_map(c, scale_row_next);
+#pragma unroll
+    for (int i = 0; i < 7; ++i) rows_lds[i * 256] = rows_next[i];
+    rows_lds[7 * 256] = scale_row_next;
+  }
+  // the tile's scales, into the half of their buffers that the tile before the last used
+  turn ^= 1;
+  {
+    const char* slot = c.slots + (size_t)done.slot * c.slot_bytes;
+    const I8Offsets off = i8_offsets((size_t)c.hidden, (size_t)c.ffn);
+    const int n_groups = (GATEUP ? 2 * c.ffn : c.hidden) / TILE_N;
+    int g = done.nt * 8 + tid_rows / 32;
+    if (g >= n_groups) g = 0;  // (never stored)
+    const float* scales = (const float*)(slot + (!GATEUP ? off.down_scales : g % 2 ? off.up_scales : off.gate_scales));
+    load_to_lds_4(row_scales + scale_row, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)&w.row_scales[turn][wave * 64]);
+    load_to_lds_4(scales + (GATEUP ? g / 2 : g) * TILE_N + tid_rows % 32,
+                  (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)&w.col_scales[turn][wave * 64]);
+  }
+  int lane_steps = lane;
+  asm volatile("" : "+v"(lane_steps));
+  auto then = [&]() __attribute__((always_inline)) {
+    int lane_then = lane;
+    asm volatile("" : "+v"(lane_then));
+    if constexpr (GATEUP) {
+#pragma unroll
+      for (int i = 0; i < 7; ++i) {
+        rows_next[i] = w.rows[i * 256 + wave * 64 + lane_then];
+        asm volatile("" : "+v"(rows_next[i]));
+      }
+    } else {
+      FULL::fetch_rows(c, loc, loc.m0, wave, lane_then, rows_next);
+    }
+    return TILE::row_sources(c, in, loc, rows_next, wave, lane_then);
+  };
+  TILE::template steps_walk<START, ODD>(TILE::row_sources(c, in, done, rows, wave, lane_steps), then, w.ring, wave, lane_steps, k_steps,
+                                        stage, ring, acc);
+  int lane_there = lane;
+  asm volatile("" : "+v"(lane_there));
+  TILE::epilogue_walk_i8(c, out, done, acc, w.staging, w.row_scales[turn], w.col_scales[turn] + wave * 64, wave, lane_there);
+  walk_wait_ring(ring);
+  // A next tile that is higher than this one: its last rows were not copied (this tile's steps copy FM row blocks).
+  if (fm > FM) {  // uniform
+    const int s0 = stage, s1 = stage + 1 == 3 ? 0 : stage + 1;
+#pragma unroll
+    for (int op = FM; op < 7; ++op)
+      if (op < fm) {
+        const typename FULL::RowSrc src = FULL::row_sources(c, in, loc, rows_next, wave, lane_there);
+        FULL::copy_to_stage(src.a_at(op, 0), lds0, wave, s0, op);
+        FULL::copy_to_stage(src.a_at(op, 8), lds0, wave, s1, op);
+      }
+    wait_vmcnt<0>();
+  }
+}
+
+// ODD: an odd number of K steps, every other tile of a block then starts in the other half of the weight ring.
+template <bool GATEUP, bool ODD, class OUT>
+__global__ __launch_bounds__(256) void ffn_tile_walk_i8_kernel(TiledCtx c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
+                                                               OUT* __restrict__ out) {
+  typedef WalkI8<GATEUP, 7> FULL;
+  __shared__ WalkI8Lds w;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)w.ring;
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  TileWalk<4> walk;
+  walk.init(c, w.table);
+  const int xcd = blockIdx.x % 8, stride = gridDim.x / 8;
+  int idx = blockIdx.x / 8;
+  TileLoc loc;
+  if (!walk.at(xcd, idx, loc)) return;  // uniform over the block
+  const int k_steps = FULL::k_units(c) / 64;
+  int rows[7];  // input rows of the thread's copies
+  u32x4 ring[8][2];
+  int fm = loc.fm, stage = 0, turn = 0;
+  FULL::fetch_rows(c, loc, loc.m0, wave, lane, rows);
+  FULL::input_rows(c, rows);
+  int scale_row = walk_scale_row(c, loc, tid);
+  if (GATEUP && c.row_map) scale_row = div_by_map(c, c.row_map[scale_row]);
+#pragma unroll
+  for (int i = 0; i < 7; ++i) w.rows[i * 256 + tid] = rows[i];
+  w.rows[7 * 256 + tid] = scale_row;
+  walk_issue_prologue<FULL>(FULL::row_sources(c, in, loc, rows, wave, lane), lds0, wave, fm, ring);
+  walk_wait_ring(ring);
+  bool more = true;
+#define HMOE_WALK_TILE(START, FM_) \
+  walk_one_tile_i8<GATEUP, ODD, START, FM_>(c, in, row_scales, out, walk, xcd, stride, wave, lane, k_steps, w, lds0, loc, idx, fm, more, \
+                                            stage, turn, ring)
+#define HMOE_WALK_HEIGHTS(START)              \
+  if (fm == 7) HMOE_WALK_TILE(START, 7);      \
+  else if (fm == 6) HMOE_WALK_TILE(START, 6); \
+  else if (fm == 5) HMOE_WALK_TILE(START, 5); \
+  else HMOE_WALK_TILE(START, 4)
+  while (more) {
+    HMOE_WALK_HEIGHTS(0);
+    if constexpr (ODD) {
+      if (!more) break;
+      HMOE_WALK_HEIGHTS(1);
+    }
+  }
+#undef HMOE_WALK_HEIGHTS
+#undef HMOE_WALK_TILE
+}
+
+enum { I8_FIT = 0, I8_FIT_PLAIN = 1, I8_FIT4 = 2, I8_FIT4_PLAIN = 3, I8_FIT256 = 4, I8_FIT256_PLAIN = 5, I8_WALK = 6 };
 
 template <bool GATEUP, class OUT>
 static void launch_stage_i8(TiledCtx c, int variant, int n_rows, const bf16_t* in, const float* row_scales, OUT* out, hipStream_t s) {
@@ -89,6 +252,18 @@ static void launch_stage_i8(TiledCtx c, int variant, int n_rows, const bf16_t* i
     hipLaunchKernelGGL(kernel, dim3((unsigned)c.grid_padded), dim3(threads), 0, s, c, in, row_scales, out);
   };
   constexpr int NW256 = GATEUP ? 8 : 4;
+  if (variant == I8_WALK) {
+    const int k_steps = (GATEUP ? c.hidden : c.ffn) / 128;
+    if (k_steps >= 6 + k_steps % 2) {
+      c.n_tiles_n = (n_total + 255) / 256;
+      c.walk_bm = 224;
+      c.grid_padded = (int)std::min(256l, (tiles_upper_bound(c, n_rows, c.walk_bm) + 7) / 8 * 8);  // one block per CU
+      const auto kernel = k_steps % 2 ? &ffn_tile_walk_i8_kernel<GATEUP, true, OUT> : &ffn_tile_walk_i8_kernel<GATEUP, false, OUT>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)c.grid_padded), dim3(256), 0, s, c, in, row_scales, out);
+      return;
+    }
+    variant = I8_FIT4_PLAIN;
+  }
   switch (variant) {
     case I8_FIT: launch(&ffn_tile_i8_kernel<GATEUP, 8, true, OUT>, 128, 512, 512); break;
     case I8_FIT_PLAIN: launch(&ffn_tile_i8_kernel<GATEUP, 8, false, OUT>, 128, 512, 512); break;
@@ -110,8 +285,8 @@ int launch_ffn_tiled_i8(const FfnArgs& a) {
   int v_gate_up = I8_FIT, v_down = I8_FIT;
   if (a.n_rows / d.n_experts >= 192) v_gate_up = v_down = I8_FIT4_PLAIN;
   if (const char* env = getenv("HMOE_I8_VARIANT")) {  // tuning: "<gate/up><down>"
-    if (env[0] >= '0' && env[0] <= '5') v_gate_up = env[0] - '0';
-    if (env[0] && env[1] >= '0' && env[1] <= '5') v_down = env[1] - '0';
+    if (env[0] >= '0' && env[0] <= '6') v_gate_up = env[0] - '0';
+    if (env[0] && env[1] >= '0' && env[1] <= '6') v_down = env[1] - '0';
   }
   launch_quantize_x_i8(a);
   probe_before(a.stream);

@@ -28,6 +28,13 @@ __device__ __forceinline__ void load_to_lds_16(const void* gptr, uint32_t lds_ba
                : "v"(gptr), "s"(__builtin_amdgcn_readfirstlane(lds_base))
                : "memory", "m0");
 }
+// One 4-byte copy per lane likewise: the wave's 64 values land at lds_base .. + 256.
+__device__ __forceinline__ void load_to_lds_4(const void* gptr, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               :
+               : "v"(gptr), "s"(__builtin_amdgcn_readfirstlane(lds_base))
+               : "memory", "m0");
+}
 // 16-byte global store issued by hand (a kernel that keeps hand-issued loads in flight across its epilogue issues
 // every vector-memory operation itself, so that the compiler never waits for, or counts, any of them)
 __device__ __forceinline__ void store_16(void* gptr, const u32x4& v) {
@@ -440,11 +447,12 @@ struct StreamTile {
   // turn issue the first loads of the NEXT tile, from the sources that `then()` returns (called when the other steps
   // are through), in place of loads this tile has no use for: they run the same code with their step numbers counted
   // from the next tile's start.  No operation changes its place in the
-  // vector-memory order, so every hand-counted wait stands.  The ring holds two K steps: k_steps must be even, and at
-  // least 6.
+  // vector-memory order, so every hand-counted wait stands.  The ring holds two K steps: START is the half of it that holds
+  // the tile's first one.  k_steps is even and at least 6, or with ODD odd and at least 7; the next tile then starts in the
+  // other half.
   // stage: the ring stage of the tile's first step, on return that of the next tile's first step.
   // On return the next tile's first loads and copies are in flight.
-  template <class THEN>
+  template <int START = 0, bool ODD = false, class THEN>
   static __device__ __forceinline__ void steps_walk(const RowSrc& now, THEN then, u32x4* lds, int wave, int lane, int k_steps,
                                                     int& stage, u32x4 (&ring)[DB][FN], Acc& acc) {
     static_assert(TR && ILV && FN == 2 && DB == 2 * KK && SA == 3, "");
@@ -475,19 +483,28 @@ struct StreamTile {
     };
     // The first two steps stand apart: the accumulators start at zero (the caller's zero_acc), so their first matrix
     // instructions take the constant as their addend and nothing has to be cleared.
-    k_step(0, std::integral_constant<int, 0>{}, now, 0);
-    k_step(1, std::integral_constant<int, 1>{}, now, 0);
+    std::integral_constant<int, START> here;
+    std::integral_constant<int, 1 - START> there;
+    k_step(0, here, now, 0);
+    k_step(1, there, now, 0);
     // (a loop that always runs: with a way round it, registers with loads in flight would meet at the far end)
     int t = 2;
 #pragma nounroll
     do {
-      k_step(t, std::integral_constant<int, 0>{}, now, 0);
-      k_step(t + 1, std::integral_constant<int, 1>{}, now, 0);
+      k_step(t, here, now, 0);
+      k_step(t + 1, there, now, 0);
       t += 2;
-    } while (t + 2 < k_steps);
-    const RowSrc after = then();
-    k_step(t, std::integral_constant<int, 0>{}, after, k_steps);
-    k_step(t + 1, std::integral_constant<int, 1>{}, after, k_steps);
+    } while (t + 2 < k_steps - (ODD ? 1 : 0));
+    if constexpr (ODD) {
+      k_step(t, here, now, 0);
+      const RowSrc after = then();
+      k_step(t + 1, there, after, k_steps);
+      k_step(t + 2, here, after, k_steps);
+    } else {
+      const RowSrc after = then();
+      k_step(t, here, after, k_steps);
+      k_step(t + 1, there, after, k_steps);
+    }
   }
   // The sources of a tile, given the input rows of its copies
   static __device__ __forceinline__ RowSrc row_sources(const TiledCtx& c, const bf16_t* __restrict__ in, const TileLoc& loc,
@@ -777,6 +794,73 @@ struct StreamTile {
       }
     }
   }
+  // The same for integer sums (NUM = StreamI8): times the scales of their rows and columns, which lie in LDS (row_scales: the
+  // tile's rows; col_scales: the wave's 64 packed columns), then SwiGLU into fp32 rows of 32 columns, or bfloat16 rows of 64:
+  // 128 bytes of a row per wave in both.
+  template <class OUT>
+  static __device__ __forceinline__ void epilogue_walk_i8(const TiledCtx& c, OUT* __restrict__ out, const TileLoc& loc, Acc& acc,
+                                                          u32x4* staging, const float* row_scales, const float* col_scales, int wave,
+                                                          int lane) {
+    static_assert(GATEUP == (sizeof(OUT) == 4), "h in fp32, o_perm in bfloat16");
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
+    const int row_first = loc.row_first, m_rows = loc.m_rows, nt = loc.nt;
+    const int n_out = GATEUP ? c.ffn : c.hidden;
+    const int m0 = loc.m0;
+    const int half = lane / 32, rl = lane % 32;
+    char* block = (char*)(staging + wave * 64 * 8);  // two [32 rows][128 bytes] halves, the wave's own
+    constexpr int PER = 16 / sizeof(OUT);
+    const int n = nt * (GATEUP ? BN / 2 : BN) + wave * 8 * PER + (lane % 8) * PER;
+    f32x4_t cs[FN][4];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) cs[j][q] = *(const f32x4_t*)(col_scales + j * 32 + q * 8 + half * 4);
+    auto write_fragment = [&](int i) {
+      const int row = (i % 2) * 32 + rl;
+      const float rs = row_scales[i * 32 + rl];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4_t v[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) v[j][t] = i8_product(acc[i][j][q * 4 + t], rs, cs[j][q][t]);
+        if constexpr (GATEUP) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) v[0][t] = silu_f32(v[0][t]) * v[1][t];
+          *(f32x4_t*)(block + staged_at(row, q * 2 + half)) = v[0];
+        } else {
+#pragma unroll
+          for (int j = 0; j < FN; ++j) {
+            uint2 pk;
+            pk.x = f32_to_bf16_pair(v[j][0], v[j][1]);
+            pk.y = f32_to_bf16_pair(v[j][2], v[j][3]);
+            *(uint2*)(block + staged_at(row, j * 4 + q) + half * 8) = pk;
+          }
+        }
+      }
+    };
+    write_fragment(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      u32x4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = *(const u32x4*)(block + staged_at((i % 2) * 32 + k * 8 + lane / 8, lane % 8));
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < FM) write_fragment(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int m = m0 + i * 32 + k * 8 + lane / 8;
+        if (m < m_rows && n < n_out) store_16(out + (size_t)(row_first + m) * n_out + n, v[k]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
   // Down projection with one weight group per wave: a wave's 32 columns are a quarter of a line.  The block collects
   // the tile's bf16 results in the idle activation ring, [rows][32 * NWV columns], and every thread stores whole
   // 16-byte pieces of whole lines.
@@ -806,5 +890,29 @@ struct StreamTile {
     }
   }
 };
+
+// Blocks that go from tile to tile (StreamTile::steps_walk): first loads and copies of a block's first tile (fm copies per thread and stage, into stages 0 and 1)
+template <class TILE>
+__device__ __forceinline__ void walk_issue_prologue(const typename TILE::RowSrc& src, uint32_t lds0, int wave, int fm,
+                                                    u32x4 (&ring)[8][2]) {
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) ring[s][j] = src.b_at(j, (size_t)s * 64);
+#pragma unroll
+  for (int st = 0; st < 2; ++st)
+#pragma unroll
+    for (int op = 0; op < 7; ++op)
+      if (op < fm) TILE::copy_to_stage(src.a_at(op, (size_t)st * 8), lds0, wave, st, op);  // uniform
+}
+// every vector-memory operation of the thread has completed; the operands tie the weight ring to the wait
+__device__ __forceinline__ void walk_wait_ring(u32x4 (&r)[8][2]) {
+  asm volatile("s_waitcnt vmcnt(0)"
+               : "+v"(r[0][0]), "+v"(r[0][1]), "+v"(r[1][0]), "+v"(r[1][1]), "+v"(r[2][0]), "+v"(r[2][1]), "+v"(r[3][0]),
+                 "+v"(r[3][1]), "+v"(r[4][0]), "+v"(r[4][1]), "+v"(r[5][0]), "+v"(r[5][1]), "+v"(r[6][0]), "+v"(r[6][1]),
+                 "+v"(r[7][0]), "+v"(r[7][1])
+               :
+               : "memory");
+}
 
 }  // namespace hmoe
