@@ -83,11 +83,11 @@ __global__ __launch_bounds__(64 * NWV) void ffn_tile256_i8_kernel(TiledCtx c, co
 // The scales of a tile's rows and columns travel to LDS with two copies issued by hand at its start; the waits of its K steps,
 // which are more than any of them leaves in flight, see them through.
 constexpr int WALK_ROWS = 8;  // per thread in LDS: the input rows of its seven copies, and the row whose scale it copies
-template <bool GATEUP, int FM>
-using WalkI8 = StreamTile<GATEUP, 224, 4, 3, false, 8, FM, 2, true, true, StreamI8>;
+template <bool GATEUP, int FM, bool NT>
+using WalkI8 = StreamTile<GATEUP, 224, 4, 3, NT, 8, FM, 2, true, true, StreamI8>;
 
 struct WalkI8Lds {
-  u32x4 ring[WalkI8<true, 7>::LDS_VEC];
+  u32x4 ring[WalkI8<true, 7, false>::LDS_VEC];
   u32x4 staging[4 * 64 * 8];
   float row_scales[2][256], col_scales[2][256];  // of the tile at hand and the next
   int table[TileWalk<4>::TABLE_INTS];
@@ -101,13 +101,13 @@ __device__ __forceinline__ int walk_scale_row(const TiledCtx& c, const TileLoc& 
 
 // One tile of fm == FM fragments whose first K step lies in half START of the weight ring.  In: loc, ring and stage describe the
 // tile, whose first loads have landed; w.rows (gate/up) its input rows.  Out: the same for the block's next tile.
-template <bool GATEUP, bool ODD, int START, int FM, class OUT>
+template <bool GATEUP, bool NT, bool ODD, int START, int FM, class OUT>
 __device__ __forceinline__ void walk_one_tile_i8(const TiledCtx& c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
                                                  OUT* __restrict__ out, const TileWalk<4>& walk, int xcd, int stride, int wave, int lane,
                                                  int k_steps, WalkI8Lds& w, uint32_t lds0, TileLoc& loc, int& idx, int& fm, bool& more,
                                                  int& stage, int& turn, u32x4 (&ring)[8][2]) {
-  typedef WalkI8<GATEUP, FM> TILE;
-  typedef WalkI8<GATEUP, 7> FULL;
+  typedef WalkI8<GATEUP, FM, NT> TILE;
+  typedef WalkI8<GATEUP, 7, NT> FULL;
   const TileLoc done = loc;
   idx += stride;
   more = walk.at(xcd, idx, loc);  // leaves loc as it is when there is no further tile
@@ -194,10 +194,10 @@ __device__ __forceinline__ void walk_one_tile_i8(const TiledCtx& c, const bf16_t
 }
 
 // ODD: an odd number of K steps, every other tile of a block then starts in the other half of the weight ring.
-template <bool GATEUP, bool ODD, class OUT>
+template <bool GATEUP, bool NT, bool ODD, class OUT>
 __global__ __launch_bounds__(256) void ffn_tile_walk_i8_kernel(TiledCtx c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
                                                                OUT* __restrict__ out) {
-  typedef WalkI8<GATEUP, 7> FULL;
+  typedef WalkI8<GATEUP, 7, NT> FULL;
   __shared__ WalkI8Lds w;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)w.ring;
   const int tid = threadIdx.x, lane = tid % 64;
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) void ffn_tile_walk_i8_kernel(TiledCtx c, const
   walk_wait_ring(ring);
   bool more = true;
 #define HMOE_WALK_TILE(START, FM_) \
-  walk_one_tile_i8<GATEUP, ODD, START, FM_>(c, in, row_scales, out, walk, xcd, stride, wave, lane, k_steps, w, lds0, loc, idx, fm, more, \
+  walk_one_tile_i8<GATEUP, NT, ODD, START, FM_>(c, in, row_scales, out, walk, xcd, stride, wave, lane, k_steps, w, lds0, loc, idx, fm, more, \
                                             stage, turn, ring)
 #define HMOE_WALK_HEIGHTS(START)              \
   if (fm == 7) HMOE_WALK_TILE(START, 7);      \
@@ -241,37 +241,59 @@ __global__ __launch_bounds__(256) void ffn_tile_walk_i8_kernel(TiledCtx c, const
 #undef HMOE_WALK_TILE
 }
 
-enum { I8_FIT = 0, I8_FIT_PLAIN = 1, I8_FIT4 = 2, I8_FIT4_PLAIN = 3, I8_FIT256 = 4, I8_FIT256_PLAIN = 5, I8_WALK = 6 };
+// Tile shapes.  nt: weight loads that are not kept in the caches.
+enum { I8_FIT4 = 0, I8_FIT256 = 1, I8_WALK = 2 };
 
 template <bool GATEUP, class OUT>
-static void launch_stage_i8(TiledCtx c, int variant, int n_rows, const bf16_t* in, const float* row_scales, OUT* out, hipStream_t s) {
+static void launch_stage_i8(TiledCtx c, int shape, bool nt, int n_rows, const bf16_t* in, const float* row_scales, OUT* out, hipStream_t s) {
   const int n_total = GATEUP ? 2 * c.ffn : c.hidden;
-  auto launch = [&](auto kernel, int bm, int bn, int threads) {
+  auto launch = [&](auto kernel, int bm, int bn, int threads, long most) {
     c.n_tiles_n = (n_total + bn - 1) / bn;
-    c.grid_padded = (int)((tiles_upper_bound(c, n_rows, bm) + 7) / 8 * 8);
+    c.grid_padded = (int)std::min(most, (tiles_upper_bound(c, n_rows, bm) + 7) / 8 * 8);
     hipLaunchKernelGGL(kernel, dim3((unsigned)c.grid_padded), dim3(threads), 0, s, c, in, row_scales, out);
   };
   constexpr int NW256 = GATEUP ? 8 : 4;
-  if (variant == I8_WALK) {
-    const int k_steps = (GATEUP ? c.hidden : c.ffn) / 128;
-    if (k_steps >= 6 + k_steps % 2) {
-      c.n_tiles_n = (n_total + 255) / 256;
-      c.walk_bm = 224;
-      c.grid_padded = (int)std::min(256l, (tiles_upper_bound(c, n_rows, c.walk_bm) + 7) / 8 * 8);  // one block per CU
-      const auto kernel = k_steps % 2 ? &ffn_tile_walk_i8_kernel<GATEUP, true, OUT> : &ffn_tile_walk_i8_kernel<GATEUP, false, OUT>;
-      hipLaunchKernelGGL(kernel, dim3((unsigned)c.grid_padded), dim3(256), 0, s, c, in, row_scales, out);
-      return;
-    }
-    variant = I8_FIT4_PLAIN;
+  constexpr long ALL = 0x7ffffff8;
+  if (shape == I8_WALK) {
+    const bool odd = (GATEUP ? c.hidden : c.ffn) / 128 % 2;
+    c.walk_bm = 224;
+    const auto kernel = odd ? (nt ? &ffn_tile_walk_i8_kernel<GATEUP, true, true, OUT> : &ffn_tile_walk_i8_kernel<GATEUP, false, true, OUT>)
+                            : (nt ? &ffn_tile_walk_i8_kernel<GATEUP, true, false, OUT> : &ffn_tile_walk_i8_kernel<GATEUP, false, false, OUT>);
+    launch(kernel, 224, 256, 256, 256);  // one block per CU
+  } else if (shape == I8_FIT256) {
+    launch(nt ? &ffn_tile256_i8_kernel<GATEUP, NW256, true, OUT> : &ffn_tile256_i8_kernel<GATEUP, NW256, false, OUT>, 256, 32 * NW256,
+           64 * NW256, ALL);
+  } else {
+    launch(nt ? &ffn_tile_i8_kernel<GATEUP, 4, true, OUT> : &ffn_tile_i8_kernel<GATEUP, 4, false, OUT>, 128, 256, 256, ALL);
   }
-  switch (variant) {
-    case I8_FIT: launch(&ffn_tile_i8_kernel<GATEUP, 8, true, OUT>, 128, 512, 512); break;
-    case I8_FIT_PLAIN: launch(&ffn_tile_i8_kernel<GATEUP, 8, false, OUT>, 128, 512, 512); break;
-    case I8_FIT4: launch(&ffn_tile_i8_kernel<GATEUP, 4, true, OUT>, 128, 256, 256); break;
-    case I8_FIT4_PLAIN: launch(&ffn_tile_i8_kernel<GATEUP, 4, false, OUT>, 128, 256, 256); break;
-    case I8_FIT256: launch(&ffn_tile256_i8_kernel<GATEUP, NW256, true, OUT>, 256, 32 * NW256, 64 * NW256); break;
-    default: launch(&ffn_tile256_i8_kernel<GATEUP, NW256, false, OUT>, 256, 32 * NW256, 64 * NW256); break;
-  }
+}
+
+// Which shape a launch takes (us; 64 experts of 2048 x 1408 top 6, 8 of 4096 x 14336 top 2, 64 of 3584 x 2560 top 8, 16 of 1024 x 640
+// top 2, rows per expert on average):
+//   * 60 rows or more (down 96): walking blocks; for a gate/up launch against the better of the other two shapes 84 / 89 and 100 /
+//     104 (66 and 140 rows of the first), 207 / 226 (128 of the second), 232 / 245 (62 of the third), 37 / 51 (1000 of the fourth); one
+//     expert of 3584 x 20480, 200 rows 41 / 50; but 20 rows of the second 167 / 157.  A down launch (66 rows of the first 49 / 44) has
+//     half the columns or fewer and needs a tile for every CU: 200 rows of the second, 128 tiles, 154 / 130; 300 rows, 256 tiles, 145 / 186.
+//   * Few tiles: up to 256 rows by 32 columns per wave, each wave of a tile then multiplies as little as it can and an
+//     expert's weights are read once: fourth, 40 tokens 11.4 / 12.4; with a long K also when there are more tiles, since a tile's
+//     time is what counts (down, 75 rows of the second 98 / 126).  But 90 experts of 768 x 768, 26 rows 42 / 30.
+//   * Else 128 x 256, two blocks per CU.
+// Weights that do not stay in the 256 MiB behind the L2s from call to call anyway are loaded past the caches while one
+// tile holds all rows of an expert (down, 4.5 rows of the first 33 / 38; 40 tokens of the fourth, in the caches, 10.0 / 9.2).
+struct I8Choice {
+  int shape;
+  bool nt;
+};
+static I8Choice choose_i8(const hmoe_layer_desc& d, int n_rows, bool gate_up) {
+  const long K = gate_up ? d.hidden : d.ffn, n_total = gate_up ? 2l * d.ffn : d.hidden;
+  const long busy = std::min(d.n_experts, n_rows), per_expert = n_rows / d.n_experts;
+  const long k_steps = K / 128;
+  const bool far = 3l * d.hidden * d.ffn * d.n_experts > (256l << 20);
+  const long walk_tiles = (n_rows / 224 + busy) * ((n_total + 255) / 256);
+  if (per_expert >= (gate_up ? 60 : 96) && k_steps >= 6 + k_steps % 2 && (gate_up || walk_tiles >= 256)) return {I8_WALK, far && per_expert <= 224};
+  const long tiles = (n_rows / 128 + busy) * ((n_total + 255) / 256);
+  if (tiles <= 128 || (tiles <= 320 && K >= 4096)) return {I8_FIT256, far && per_expert <= 192};
+  return {I8_FIT4, far && per_expert <= 96};
 }
 
 int launch_ffn_tiled_i8(const FfnArgs& a) {
@@ -282,19 +304,23 @@ int launch_ffn_tiled_i8(const FfnArgs& a) {
   const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
   const bf16_t* codes = (const bf16_t*)((const char*)a.h + w.codes);
   const float* scales = (const float*)((const char*)a.h + w.scales);
-  int v_gate_up = I8_FIT, v_down = I8_FIT;
-  if (a.n_rows / d.n_experts >= 192) v_gate_up = v_down = I8_FIT4_PLAIN;
-  if (const char* env = getenv("HMOE_I8_VARIANT")) {  // tuning: "<gate/up><down>"
-    if (env[0] >= '0' && env[0] <= '6') v_gate_up = env[0] - '0';
-    if (env[0] && env[1] >= '0' && env[1] <= '6') v_down = env[1] - '0';
+  I8Choice gate_up = choose_i8(d, a.n_rows, true), down = choose_i8(d, a.n_rows, false);
+  if (const char* env = getenv("HMOE_I8_TILES")) {  // tuning and tests: "<gate/up><down>", 0 .. 2 the shapes, 3 .. 5 the same past the caches
+    auto forced = [](char c, int k, I8Choice otherwise) {
+      const int v = c - '0';
+      if (v < 0 || v > 5 || (v % 3 == I8_WALK && k / 128 < 6 + k / 128 % 2)) return otherwise;
+      return I8Choice{v % 3, v >= 3};
+    };
+    gate_up = forced(env[0], d.hidden, gate_up);
+    if (env[0]) down = forced(env[1], d.ffn, down);
   }
   launch_quantize_x_i8(a);
   probe_before(a.stream);
-  launch_stage_i8<true>(c, v_gate_up, a.n_rows, codes, scales, (float*)a.h, a.stream);
+  launch_stage_i8<true>(c, gate_up.shape, gate_up.nt, a.n_rows, codes, scales, (float*)a.h, a.stream);
   probe_after(a.stream);
   launch_quantize_h_i8(a);
   probe_before(a.stream);
-  launch_stage_i8<false>(c, v_down, a.n_rows, codes, scales, (bf16_t*)a.o_perm, a.stream);
+  launch_stage_i8<false>(c, down.shape, down.nt, a.n_rows, codes, scales, (bf16_t*)a.o_perm, a.stream);
   probe_after(a.stream);
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;

@@ -299,3 +299,46 @@ def test_a_prefill_batch_of_many_tiles(hm):
     again = grouped(hm, d, layer, to_device(x), to_device(offsets), A, 0)
     assert torch.equal(o.view(torch.int16), again.view(torch.int16))
     layer.close()
+
+
+@pytest.mark.parametrize("tiles", ["00", "11", "22", "33", "44", "55"])
+@pytest.mark.parametrize("hidden,ffn,counts", [
+    (768, 896, [700, 1, 0, 224, 225, 31]),       # 6 and 7 K steps: an even and an odd number, the fewest of walking blocks
+    (896, 1152, [97, 300, 448, 33, 64, 0]),      # 7 and 9
+    (1024, 1408, [130] * 9),                     # 8 and 11
+    (2304, 768, [256, 129]),                     # 18 and 6
+])
+def test_every_tile_shape(hm, monkeypatch, tiles, hidden, ffn, counts):
+    """Each tile shape of the prefill kernels, with and without weights that pass the caches; the same bits from all of them."""
+    say("i8 tiles", tiles, hidden, ffn, counts)
+    d, experts, layer = make(hm, hidden, ffn, len(counts), 1, hidden, distinct=2)
+    offsets = offsets_of(counts)
+    A = int(offsets[-1])
+    x = rows_of(8, A, hidden)
+    args = (hm, d, layer, to_device(x), to_device(offsets), A, TILED)
+    want = grouped(*args)
+    monkeypatch.setenv("HMOE_I8_TILES", tiles)
+    got = grouped(*args)
+    assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+    some = np.r_[0:8, A - 8:A]                     # (the oracle: a few rows of the first and the last expert with rows)
+    own = np.concatenate([np.full(n, e) for e, n in enumerate(counts)])[some]
+    for e in set(own):
+        ref, slack = i8.expert_ffn(wl.as_f64(x[some[own == e]]), *(wl.as_f64(m) for m in experts[e]))
+        err = np.abs(to_host_f32(got)[some[own == e]] - ref)
+        assert (err <= slack + 2.0 ** -8 * (np.abs(ref) + slack)).all()
+    layer.close()
+
+
+def test_walking_blocks_with_many_tiles_each(hm, monkeypatch):
+    """Hundreds of tiles of mixed heights: every block of the launch goes through several, in both halves of its weight ring."""
+    say("i8 walk, many tiles")
+    counts = [40, 300, 224, 500, 97, 161, 193, 1000] * 4
+    d, experts, layer = make(hm, 896, 2688, len(counts), 1, 5, distinct=1)
+    x = to_device(rows_of(9, sum(counts), 896))
+    args = (hm, d, layer, x, to_device(offsets_of(counts)), sum(counts), TILED)
+    monkeypatch.setenv("HMOE_I8_TILES", "00")
+    want = grouped(*args)
+    monkeypatch.setenv("HMOE_I8_TILES", "22")
+    for _ in range(3):
+        assert torch.equal(grouped(*args).view(torch.int16), want.view(torch.int16))
+    layer.close()
