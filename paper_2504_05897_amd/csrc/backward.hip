@@ -116,8 +116,9 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const int32_t* __re
     const int e = e0 + l;
     float v = 0.0f;
     for (int j = 0; j < top_k; ++j) {
-      const int named = __shfl(id, j, G);
-      const float part = __shfl(own, j, G);
+      // (a token per wavefront: through scalar registers)
+      const int named = G == 64 ? __builtin_amdgcn_readlane(id, j) : __shfl(id, j, G);
+      const float part = G == 64 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), j)) : __shfl(own, j, G);
       if (named == e) v += part;
     }
     if (e < n_experts) d_logits[(size_t)t * n_experts + e] = v;
@@ -168,23 +169,35 @@ __device__ __forceinline__ f32x4_t mfma_16x16x4_f32(float a, float b, f32x4_t c)
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-constexpr int RB_WAVES = 4;
-constexpr int DX_COLS_BF16 = 128, DX_COLS_F32 = 64;  // columns of a wave: 16 pieces of 16 bytes
+// Number formats: columns of a wave (16 pieces of 16 bytes), values per piece, tokens of a d_w_g step.
+struct DwBf16 {
+  typedef bf16_t T;
+  static constexpr int COLS = 128, PIECE = 8, STEP = 32;
+};
+struct DwF32 {
+  typedef float T;
+  static constexpr int COLS = 64, PIECE = 4, STEP = 16;
+};
 
-// dx, bfloat16: a wave takes 16 RF tokens x 128 columns and goes through the experts 32 at a time.
+// dx, bfloat16: a wave takes 16 RF tokens from t0 x 128 columns (slice) and goes through the experts 32 at a time.
 template <int RF>
-__global__ __launch_bounds__(64 * RB_WAVES) void router_dx_bf16_kernel(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits,
-                                                                       const bf16_t* add, int n_tokens, int n_experts, int hidden, bf16_t* dx) {
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
-  const int t0 = (blockIdx.x * RB_WAVES + wave) * 16 * RF;
-  const int col = blockIdx.y * DX_COLS_BF16 + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
-  if (t0 >= n_tokens) return;
+__device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits, const bf16_t* add,
+                                               int n_tokens, int n_experts, int hidden, bf16_t* dx, int t0, int slice) {
+  const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int col = slice * DwBf16::COLS + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
   const bool whole = n_experts % 4 == 0;
   f32x4_t acc[RF][8];
 #pragma unroll
   for (int f = 0; f < RF; ++f)
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[f][i] = f32x4_t{0, 0, 0, 0};
+  u32x4 more[RF][4];  // `add`, on its way while the experts are multiplied
+  if (add) {
+#pragma unroll
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) more[f][r] = *(const u32x4*)(add + (size_t)min(t0 + 16 * f + 4 * kblk + r, n_tokens - 1) * hidden + col_at);
+  }
   for (int e0 = 0; e0 < n_experts; e0 += 32) {
     const int e = e0 + 8 * kblk;
     u32x4 w[8], op[8];
@@ -227,26 +240,22 @@ __global__ __launch_bounds__(64 * RB_WAVES) void router_dx_bf16_kernel(const bf1
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = acc[f][i][r];
       if (add) {
-        const u32x4 s = *(const u32x4*)(add + (size_t)t * hidden + col);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          v[2 * i] += __uint_as_float(s[i] << 16);
-          v[2 * i + 1] += __uint_as_float(s[i] & 0xffff0000u);
+          v[2 * i] += __uint_as_float(more[f][r][i] << 16);
+          v[2 * i + 1] += __uint_as_float(more[f][r][i] & 0xffff0000u);
         }
       }
       *(u32x4*)(dx + (size_t)t * hidden + col) = round_piece(v);
     }
 }
 
-// dx, fp32: a wave takes 16 RF tokens x 64 columns and goes through the experts 16 at a time; instruction s of a step has
-// experts 4 (l / 16) + s.
+// dx, fp32: 16 RF tokens x 64 columns, the experts 16 at a time; instruction s of a step has experts 4 (l / 16) + s.
 template <int RF>
-__global__ __launch_bounds__(64 * RB_WAVES) void router_dx_f32_kernel(const float* __restrict__ w_g, const float* __restrict__ d_logits,
-                                                                      const float* add, int n_tokens, int n_experts, int hidden, float* dx) {
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
-  const int t0 = (blockIdx.x * RB_WAVES + wave) * 16 * RF;
-  const int col = blockIdx.y * DX_COLS_F32 + 4 * n;
-  if (t0 >= n_tokens) return;
+__device__ __forceinline__ void router_dx_wave(const float* __restrict__ w_g, const float* __restrict__ d_logits, const float* add, int n_tokens,
+                                               int n_experts, int hidden, float* dx, int t0, int slice) {
+  const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int col = slice * DwF32::COLS + 4 * n;
   const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
   f32x4_t acc[RF][4];
 #pragma unroll
@@ -285,38 +294,57 @@ __global__ __launch_bounds__(64 * RB_WAVES) void router_dx_f32_kernel(const floa
     }
 }
 
-// d_w_g: a block takes 64 experts x DwShape::COLS columns over one chunk of the tokens, each of its waves every fourth step of
-// STEP tokens; the waves' sums meet in LDS, the chunks' in router_dw_sum_kernel, all in a fixed order.
-struct DwBf16 {
-  typedef bf16_t T;
-  static constexpr int COLS = 128, STEP = 32, PIECE = 8;
-};
-struct DwF32 {
-  typedef float T;
-  static constexpr int COLS = 64, STEP = 16, PIECE = 4;
-};
-constexpr int DW_EXPERTS = 64;
+// dx of large batches: four waves per block
+template <class NUM, int RF>
+__global__ __launch_bounds__(256, RF == 1 ? 4 : 3) void router_dx_kernel(const typename NUM::T* __restrict__ w_g, const float* __restrict__ d_logits,
+                                                                         const typename NUM::T* add, int n_tokens, int n_experts, int hidden,
+                                                                         typename NUM::T* dx) {
+  const int t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 16 * RF;
+  if (t0 < n_tokens) router_dx_wave<RF>(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, blockIdx.y);
+}
 
-// the operands of a step: tokens t .. + 8 of the lane's k block
-struct DwStepBf16 {
+// d_w_g: a block takes 16 M experts x NUM::COLS columns over some of the tokens, each of its eight waves every eighth step of
+// STEP tokens.  The waves' sums meet in LDS, the blocks' of several chunks of the tokens in router_dw_sum_kernel, all in a
+// fixed order.  M = 4: a step's x serves 64 experts; M = 1: four times the blocks, for batches that make few.
+//
+// The operands of a step.  Tokens past the end are cleared where they are multiplied, in the step that has some: behind the
+// loads it would be a wait for them.  Operand m of lane n has expert e + m, e = e0 + M n.
+template <class NUM, int M>
+struct DwStep;
+template <int M>
+__device__ __forceinline__ void load_logits(float (&v)[M], const float* row, int e, int n_experts, bool whole) {
+  if constexpr (M == 4) {
+    const f32x4_t q = load_4(row, e, n_experts, whole);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) v[m] = q[m];
+  } else {
+    v[0] = e < n_experts ? row[e] : 0.0f;
+  }
+}
+template <int M>
+struct DwStep<DwBf16, M> {
   u32x4 x[8];
-  f32x4_t d[8];
+  float d[8][M];
   __device__ __forceinline__ void load(const bf16_t* __restrict__ x_in, const float* __restrict__ d_logits, int t0, int t_end, int col_at,
                                        int e, int n_experts, int hidden, bool whole_e, bool, int kblk) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const int t = t0 + 8 * kblk + k, at = min(t, t_end - 1);
+      const int at = min(t0 + 8 * kblk + k, t_end - 1);
       x[k] = *(const u32x4*)(x_in + (size_t)at * hidden + col_at);
-      d[k] = load_4(d_logits + (size_t)at * n_experts, e, n_experts, whole_e);
+      load_logits<M>(d[k], d_logits + (size_t)at * n_experts, e, n_experts, whole_e);
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)  // (both: zero times an infinity is none)
-      if (t0 + 8 * kblk + k >= t_end) {
-        x[k] = u32x4{0, 0, 0, 0};
-        d[k] = f32x4_t{0, 0, 0, 0};
-      }
   }
-  __device__ __forceinline__ void multiply(f32x4_t (&acc)[4][8]) const {
+  // left: tokens from t0 to the end
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[M][8], int left, int kblk) {
+    if (left < DwBf16::STEP) {  // uniform
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (8 * kblk + k >= left) {  // (both: zero times an infinity is none)
+          x[k] = u32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int m = 0; m < M; ++m) d[k][m] = 0.0f;
+        }
+    }
     u32x4 op[8];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -324,7 +352,7 @@ struct DwStepBf16 {
       transpose_halves(rows, op[2 * p], op[2 * p + 1]);
     }
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
+    for (int m = 0; m < M; ++m) {
       float v[8] = {d[0][m], d[1][m], d[2][m], d[3][m], d[4][m], d[5][m], d[6][m], d[7][m]};
 #pragma unroll
       for (int piece = 0; piece < 3; ++piece) {
@@ -335,90 +363,135 @@ struct DwStepBf16 {
     }
   }
 };
-struct DwStepF32 {
-  f32x4_t x[4], d[4];
+template <int M>
+struct DwStep<DwF32, M> {
+  f32x4_t x[4];
+  float d[4][M];
   __device__ __forceinline__ void load(const float* __restrict__ x_in, const float* __restrict__ d_logits, int t0, int t_end, int col_at, int e,
                                        int n_experts, int hidden, bool whole_e, bool whole_h, int kblk) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int t = t0 + 4 * k + kblk;
-      const bool there = t < t_end;
-      x[k] = there ? load_4(x_in + (size_t)t * hidden, col_at, hidden, whole_h) : f32x4_t{0, 0, 0, 0};
-      d[k] = there ? load_4(d_logits + (size_t)t * n_experts, e, n_experts, whole_e) : f32x4_t{0, 0, 0, 0};
+      const int at = min(t0 + 4 * k + kblk, t_end - 1);
+      x[k] = load_4(x_in + (size_t)at * hidden, col_at, hidden, whole_h);
+      load_logits<M>(d[k], d_logits + (size_t)at * n_experts, e, n_experts, whole_e);
     }
   }
-  __device__ __forceinline__ void multiply(f32x4_t (&acc)[4][4]) const {
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[M][4], int left, int kblk) {
+    if (left < DwF32::STEP) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (4 * k + kblk >= left) {
+          x[k] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+          for (int m = 0; m < M; ++m) d[k][m] = 0.0f;
+        }
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
+      for (int m = 0; m < M; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[m][i] = mfma_16x16x4_f32(d[k][m], x[k][i], acc[m][i]);
   }
 };
 
-template <class SHAPE, class DW_STEP>
-__global__ __launch_bounds__(64 * RB_WAVES) void router_dw_kernel(const typename SHAPE::T* __restrict__ x, const float* __restrict__ d_logits,
-                                                                     int n_tokens, int n_experts, int hidden, int chunk_tokens,
-                                                                     float* __restrict__ out) {
-  constexpr int PIECE = SHAPE::PIECE;
-  __shared__ float red[RB_WAVES][PIECE * 4][64];
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
-  const int col = blockIdx.x * SHAPE::COLS + PIECE * n;
-  const int col_at = SHAPE::PIECE == 8 ? min(col, hidden - 8) : col;  // (fp32 rows of any length are checked where they are read)
-  const int t_begin = blockIdx.y * chunk_tokens, t_end = min(t_begin + chunk_tokens, n_tokens);
-  const int e0 = blockIdx.z * DW_EXPERTS, e = e0 + 4 * n;  // operand m of the lane: expert e0 + 4 n + m
+constexpr int DW_WAVES = 8;  // two per SIMD: one multiplies while the other's step is on its way
+template <class NUM>
+using DwRed = float[DW_WAVES][NUM::PIECE * 4][64];
+
+// experts 16 M tile .., columns of `slice`, tokens t_begin .. t_end -> out [E, H]
+template <class NUM, int M>
+__device__ __forceinline__ void router_dw_block(const typename NUM::T* __restrict__ x, const float* __restrict__ d_logits, int n_experts,
+                                                int hidden, int slice, int tile, int t_begin, int t_end, float* __restrict__ out,
+                                                DwRed<NUM>& red) {
+  constexpr int PIECE = NUM::PIECE;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int col = slice * NUM::COLS + PIECE * n;
+  const int col_at = PIECE == 8 ? min(col, hidden - 8) : col;  // (fp32 rows of any length are checked where they are read)
+  const int e0 = 16 * M * tile, e = e0 + M * n;
   const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
-  f32x4_t acc[4][PIECE];
+  f32x4_t acc[M][PIECE];
 #pragma unroll
-  for (int m = 0; m < 4; ++m)
+  for (int m = 0; m < M; ++m)
 #pragma unroll
     for (int i = 0; i < PIECE; ++i) acc[m][i] = f32x4_t{0, 0, 0, 0};
-  DW_STEP step;
-  int t = t_begin + wave * SHAPE::STEP;
-  if (t < t_end) {
-    step.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
-    for (;;) {
-      const DW_STEP now = step;
-      t += RB_WAVES * SHAPE::STEP;
-      if (t >= t_end) {
-        now.multiply(acc);
-        break;
+  constexpr int STRIDE = DW_WAVES * NUM::STEP;
+  int t = t_begin + wave * NUM::STEP;
+  if constexpr (M == 1) {  // few blocks: the next step is on its way too
+    if (t < t_end) {
+      DwStep<NUM, M> ahead;
+      ahead.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
+      for (; t < t_end; t += STRIDE) {
+        DwStep<NUM, M> step = ahead;
+        if (t + STRIDE < t_end) ahead.load(x, d_logits, t + STRIDE, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
+        step.multiply(acc, t_end - t, kblk);
       }
+    }
+  } else {
+    for (; t < t_end; t += STRIDE) {
+      DwStep<NUM, M> step;
       step.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
-      now.multiply(acc);
+      step.multiply(acc, t_end - t, kblk);
     }
   }
-  // register r of lane (n, kblk) is row 4 kblk + r of the instruction: expert e0 + 4 (4 kblk + r) + m; operand i column PIECE n + i
-  out += (size_t)blockIdx.y * n_experts * hidden;
+  // register r of lane (n, kblk) is row 4 kblk + r of the instruction: expert e0 + M (4 kblk + r) + m; operand i column PIECE n + i
 #pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    __syncthreads();
+  for (int m = 0; m < M; ++m) {
+    if (m > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < PIECE; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) red[wave][i * 4 + r][lane] = acc[m][i][r];
     __syncthreads();
-    const int r = wave, to = e0 + 4 * (4 * kblk + r) + m;  // a thread per row and piece of columns
-    static_assert(RB_WAVES == 4, "");
-    float v[PIECE];
+    // a thread per row and half of its piece of columns
+    constexpr int HALF = PIECE / 2;
+    static_assert(DW_WAVES == 8, "");
+    const int r = wave % 4, i0 = wave / 4 * HALF, to = e0 + M * (4 * kblk + r) + m;
+    float v[HALF];
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) {
-      v[i] = red[0][i * 4 + r][lane];
+    for (int i = 0; i < HALF; ++i) {
+      v[i] = red[0][(i0 + i) * 4 + r][lane];
 #pragma unroll
-      for (int w = 1; w < RB_WAVES; ++w) v[i] += red[w][i * 4 + r][lane];
+      for (int w = 1; w < DW_WAVES; ++w) v[i] += red[w][(i0 + i) * 4 + r][lane];
     }
     if (to < n_experts) {
-      float* row = out + (size_t)to * hidden + col;
+      float* row = out + (size_t)to * hidden;
+      if (PIECE == 8) {  // (columns come in eights)
+        if (col < hidden) *(f32x4_t*)(row + col + i0) = f32x4_t{v[0], v[1], v[2 % HALF], v[3 % HALF]};
+      } else {
 #pragma unroll
-      for (int i = 0; i < PIECE; i += 4) {
-        if (whole_h && col + i < hidden) *(f32x4_t*)(row + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
-        else
-#pragma unroll
-          for (int k = i; k < i + 4; ++k)
-            if (col + k < hidden) row[k] = v[k];
+        for (int i = 0; i < HALF; ++i)
+          if (col + i0 + i < hidden) row[col + i0 + i] = v[i];
       }
     }
+  }
+}
+
+template <class NUM>
+__global__ __launch_bounds__(64 * DW_WAVES, 2) void router_dw_kernel(const typename NUM::T* __restrict__ x, const float* __restrict__ d_logits,
+                                                                     int n_tokens, int n_experts, int hidden, int chunk_tokens,
+                                                                     float* __restrict__ out) {
+  __shared__ DwRed<NUM> red;
+  const int t_begin = blockIdx.y * chunk_tokens;
+  router_dw_block<NUM, 4>(x, d_logits, n_experts, hidden, blockIdx.x, blockIdx.z, t_begin, min(t_begin + chunk_tokens, n_tokens),
+                          out + (size_t)blockIdx.y * n_experts * hidden, red);
+}
+
+// Batches of up to SMALL_TOKENS: both results in one launch, d_w_g without chunks.  The first dw_blocks blocks are d_w_g's (they
+// take longest), the others eight waves of dx.
+template <class NUM>
+__global__ __launch_bounds__(64 * DW_WAVES, 2) void router_backward_small_kernel(const typename NUM::T* __restrict__ x,
+                                                                                 const typename NUM::T* __restrict__ w_g,
+                                                                                 const float* __restrict__ d_logits, int n_tokens, int n_experts,
+                                                                                 int hidden, const typename NUM::T* add, typename NUM::T* dx,
+                                                                                 float* __restrict__ d_w_g, int slices, int dw_blocks) {
+  __shared__ DwRed<NUM> red;
+  const int b = blockIdx.x;
+  if (b < dw_blocks) {
+    router_dw_block<NUM, 1>(x, d_logits, n_experts, hidden, b % slices, b / slices, 0, n_tokens, d_w_g, red);
+  } else {
+    const int i = b - dw_blocks, t0 = (i / slices * DW_WAVES + threadIdx.x / 64) * 16;
+    if (t0 < n_tokens) router_dx_wave<1>(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, i % slices);
   }
 }
 
@@ -440,20 +513,51 @@ __global__ __launch_bounds__(256) void router_dw_sum_kernel(const float* __restr
   }
 }
 
-// Chunks of the tokens in the d_w_g launch: as many as give every CU a block, of 128 tokens or more.
+// Up to this many tokens one launch does everything (1003 tokens, 64 experts of 2048: SEE_BELOW).
+constexpr int SMALL_TOKENS = 2048;
+// Beyond: chunks of the tokens in the d_w_g launch, as many as give every CU a block.
 struct DwPlan {
-  int columns, expert_tiles, chunks, chunk_tokens;
+  int slices, tiles, chunks, chunk_tokens;
 };
 static DwPlan dw_plan(const hmoe_layer_desc& d, int T) {
   DwPlan p;
   const int cols = d.dtype == HMOE_F32 ? DwF32::COLS : DwBf16::COLS;
-  p.columns = (d.hidden + cols - 1) / cols;
-  p.expert_tiles = (d.n_experts + DW_EXPERTS - 1) / DW_EXPERTS;
-  const long blocks = (long)p.columns * p.expert_tiles;
-  const int want = (int)std::max(1l, std::min(256 / blocks, (long)(T + 127) / 128));
-  p.chunk_tokens = std::max(1, ((T + want - 1) / want + 127) / 128 * 128);
+  p.slices = (d.hidden + cols - 1) / cols;
+  p.tiles = (d.n_experts + 63) / 64;
+  const long blocks = (long)p.slices * p.tiles;
+  const int want = T <= SMALL_TOKENS ? 1 : (int)std::max(1l, std::min(256 / blocks, (long)(T + 255) / 256));
+  p.chunk_tokens = std::max(1, ((T + want - 1) / want + 255) / 256 * 256);
   p.chunks = std::max(1, (T + p.chunk_tokens - 1) / p.chunk_tokens);
   return p;
+}
+
+template <class NUM>
+static void launch_router_backward(const hmoe_layer_desc& d, const typename NUM::T* x, const typename NUM::T* w_g, const float* d_logits, int T,
+                                   const typename NUM::T* add, typename NUM::T* dx, float* d_w_g, float* workspace, hipStream_t s) {
+  const int E = d.n_experts, H = d.hidden;
+  const DwPlan p = dw_plan(d, T);
+  if (T <= SMALL_TOKENS) {
+    const int dw_blocks = d_w_g ? p.slices * ((E + 15) / 16) : 0, dx_blocks = dx ? p.slices * ((T + 16 * DW_WAVES - 1) / (16 * DW_WAVES)) : 0;
+    if (dw_blocks + dx_blocks > 0)
+      hipLaunchKernelGGL(router_backward_small_kernel<NUM>, dim3((unsigned)(dw_blocks + dx_blocks)), dim3(64 * DW_WAVES), 0, s, x, w_g, d_logits,
+                         T, E, H, add, dx, d_w_g, p.slices, dw_blocks);
+    return;
+  }
+  if (dx) {
+    // 32 tokens per wave where that leaves every SIMD two, else 16
+    const bool two = (long)p.slices * (T / 32) >= 2048;
+    const dim3 grid((unsigned)((T + (two ? 127 : 63)) / (two ? 128 : 64)), (unsigned)p.slices);
+    hipLaunchKernelGGL((two ? &router_dx_kernel<NUM, 2> : &router_dx_kernel<NUM, 1>), grid, dim3(256), 0, s, w_g, d_logits, add, T, E, H, dx);
+  }
+  if (d_w_g) {
+    const dim3 grid((unsigned)p.slices, (unsigned)p.chunks, (unsigned)p.tiles);
+    hipLaunchKernelGGL(router_dw_kernel<NUM>, grid, dim3(64 * DW_WAVES), 0, s, x, d_logits, T, E, H, p.chunk_tokens,
+                       p.chunks > 1 ? workspace : d_w_g);
+    if (p.chunks > 1) {
+      const long n = (long)E * H;
+      hipLaunchKernelGGL(router_dw_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, workspace, p.chunks, n, d_w_g);
+    }
+  }
 }
 
 }  // namespace hmoe
@@ -520,43 +624,20 @@ extern "C" int32_t hmoe_router_backward(const hmoe_layer_desc* desc, const void*
                                         const void* add, void* dx, float* d_w_g, void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_desc(desc);
   if (rc != HMOE_OK) return rc;
-  const int E = desc->n_experts, H = desc->hidden;
   if (T < 0 || T > 0x7fffffff / desc->top_k || T > 0x7fff0000) return HMOE_ERR_INVALID_ARG;  // (token numbers past the last tile fit)
   if (!dx && !d_w_g) return HMOE_ERR_INVALID_ARG;
   if (T > 0 && (!d_logits || (dx && !w_g) || (d_w_g && !x))) return HMOE_ERR_INVALID_ARG;
   if (!aligned16(d_logits) || (dx && (!aligned16(dx) || !aligned16(w_g) || !aligned16(add))) || (d_w_g && (!aligned16(d_w_g) || !aligned16(x))))
     return HMOE_ERR_INVALID_ARG;
-  if (desc->dtype != HMOE_F32 && H % 16 != 0) return HMOE_ERR_UNSUPPORTED;
+  if (desc->dtype != HMOE_F32 && desc->hidden % 16 != 0) return HMOE_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < hmoe_router_backward_workspace_bytes(desc, T)) return HMOE_ERR_WORKSPACE;
   if (!aligned16(workspace)) return HMOE_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
-  const bool f32 = desc->dtype == HMOE_F32;
-  if (dx && T > 0) {
-    const int columns = f32 ? DX_COLS_F32 : DX_COLS_BF16, slices = (H + columns - 1) / columns;
-    // 64 tokens per wave where that leaves every SIMD one, else 16
-    const int rf = (long)slices * (T / 64) >= 1024 ? 4 : 1;
-    const dim3 grid((unsigned)((T + 16l * rf * RB_WAVES - 1) / (16l * rf * RB_WAVES)), (unsigned)slices);
-    auto launch = [&](auto kernel, auto type) {
-      typedef decltype(type) V;
-      hipLaunchKernelGGL(kernel, grid, dim3(64 * RB_WAVES), 0, s, (const V*)w_g, d_logits, (const V*)add, T, E, H, (V*)dx);
-    };
-    if (f32) launch(rf == 4 ? &router_dx_f32_kernel<4> : &router_dx_f32_kernel<1>, 0.0f);
-    else launch(rf == 4 ? &router_dx_bf16_kernel<4> : &router_dx_bf16_kernel<1>, bf16_t{});
-  }
-  if (d_w_g) {
-    const DwPlan p = dw_plan(*desc, T);
-    float* out = p.chunks > 1 ? (float*)workspace : d_w_g;
-    const dim3 grid((unsigned)p.columns, (unsigned)p.chunks, (unsigned)p.expert_tiles);
-    if (f32)
-      hipLaunchKernelGGL((router_dw_kernel<DwF32, DwStepF32>), grid, dim3(64 * RB_WAVES), 0, s, (const float*)x, d_logits, T, E, H, p.chunk_tokens, out);
-    else
-      hipLaunchKernelGGL((router_dw_kernel<DwBf16, DwStepBf16>), grid, dim3(64 * RB_WAVES), 0, s, (const bf16_t*)x, d_logits, T, E, H,
-                         p.chunk_tokens, out);
-    if (p.chunks > 1) {
-      const long n = (long)E * H;
-      hipLaunchKernelGGL(router_dw_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, (const float*)workspace, p.chunks, n, d_w_g);
-    }
-  }
+  if (desc->dtype == HMOE_F32)
+    launch_router_backward<DwF32>(*desc, (const float*)x, (const float*)w_g, d_logits, T, (const float*)add, (float*)dx, d_w_g, (float*)workspace, s);
+  else
+    launch_router_backward<DwBf16>(*desc, (const bf16_t*)x, (const bf16_t*)w_g, d_logits, T, (const bf16_t*)add, (bf16_t*)dx, d_w_g,
+                                   (float*)workspace, s);
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;
 }
