@@ -549,6 +549,7 @@ static int32_t ffn_prepare(const hmoe_layer_desc* desc, hmoe_cache* cache, const
       // (layers of 8 experts of 4096 x 14336, 64 of 2048 x 1408 and 16 of 2048 x 1024; decode kernel -> tiles): 24 tokens
       // 169 -> 149, 89 -> 85 and 44 -> 43 us, 50 tokens 277 -> 173, 100 -> 88 and 51 -> 46 us; with 16 the third is even.
       *path = (A / desc->top_k <= 16) ? HMOE_FFN_SKINNY : HMOE_FFN_TILED;
+    else if (desc->dtype == HMOE_BF16_I8) *path = ffn_skinny_i8_takes(*desc, A) ? HMOE_FFN_SKINNY : HMOE_FFN_TILED;
     else *path = (A / desc->top_k <= 32) ? HMOE_FFN_SKINNY : HMOE_FFN_TILED;
   }
   if (desc->dtype == HMOE_F32 && *path != HMOE_FFN_REFERENCE && *path != FFN_F32_TILES) return HMOE_ERR_UNSUPPORTED;

@@ -179,128 +179,109 @@ struct DwF32 {
   static constexpr int COLS = 64, PIECE = 4, STEP = 16;
 };
 
-// dx, bfloat16: a wave takes 16 RF tokens from t0 x 128 columns (slice) and goes through the experts 32 at a time.
-template <int RF>
+// dx, bfloat16: a wave takes 16 tokens from t0 x 128 columns (slice) and goes through the experts 32 at a time.  (32 tokens for
+// each load of W_g: 69 against 68 us for gates and router of 16384 tokens; the more waves that fit hide more.)
 __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits, const bf16_t* add,
                                                int n_tokens, int n_experts, int hidden, bf16_t* dx, int t0, int slice) {
   const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
   const int col = slice * DwBf16::COLS + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
   const bool whole = n_experts % 4 == 0;
-  f32x4_t acc[RF][8];
+  f32x4_t acc[8];
 #pragma unroll
-  for (int f = 0; f < RF; ++f)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[f][i] = f32x4_t{0, 0, 0, 0};
-  u32x4 more[RF][4];  // `add`, on its way while the experts are multiplied
+  for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
+  u32x4 more[4];  // `add`, on its way while the experts are multiplied
   if (add) {
 #pragma unroll
-    for (int f = 0; f < RF; ++f)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) more[f][r] = *(const u32x4*)(add + (size_t)min(t0 + 16 * f + 4 * kblk + r, n_tokens - 1) * hidden + col_at);
+    for (int r = 0; r < 4; ++r) more[r] = *(const u32x4*)(add + (size_t)min(t0 + 4 * kblk + r, n_tokens - 1) * hidden + col_at);
   }
+  const float* row = d_logits + (size_t)min(t0 + n, n_tokens - 1) * n_experts;
   for (int e0 = 0; e0 < n_experts; e0 += 32) {
     const int e = e0 + 8 * kblk;
     u32x4 w[8], op[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) w[k] = *(const u32x4*)(w_g + (size_t)min(e + k, n_experts - 1) * hidden + col_at);
-    f32x4_t d[RF][2];
+    const f32x4_t d0 = load_4(row, e, n_experts, whole), d1 = load_4(row, e + 4, n_experts, whole);
+    if (e0 + 32 > n_experts) {  // uniform
 #pragma unroll
-    for (int f = 0; f < RF; ++f) {
-      const float* row = d_logits + (size_t)min(t0 + 16 * f + n, n_tokens - 1) * n_experts;
-      d[f][0] = load_4(row, e, n_experts, whole);
-      d[f][1] = load_4(row, e + 4, n_experts, whole);
+      for (int k = 0; k < 8; ++k)  // (a row of W_g past the last would meet zeros, but may hold an infinity)
+        if (e + k >= n_experts) w[k] = u32x4{0, 0, 0, 0};
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)  // (a row of W_g past the last would meet zeros, but may hold an infinity)
-      if (e + k >= n_experts) w[k] = u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       const uint32_t rows[8] = {w[0][p], w[1][p], w[2][p], w[3][p], w[4][p], w[5][p], w[6][p], w[7][p]};
       transpose_halves(rows, op[2 * p], op[2 * p + 1]);
     }
+    float v[8] = {d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+    const u32x4 hi = take_piece(v), lo = round_piece(v);
 #pragma unroll
-    for (int f = 0; f < RF; ++f) {
-      float v[8] = {d[f][0][0], d[f][0][1], d[f][0][2], d[f][0][3], d[f][1][0], d[f][1][1], d[f][1][2], d[f][1][3]};
-      const u32x4 hi = take_piece(v), lo = round_piece(v);
+    for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(hi, op[i], acc[i]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[f][i] = mfma_16x16x32_bf16(hi, op[i], acc[f][i]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[f][i] = mfma_16x16x32_bf16(lo, op[i], acc[f][i]);
-    }
+    for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(lo, op[i], acc[i]);
   }
-  // register r of lane (n, kblk) is token 4 kblk + r of its fragment, operand i column 8 n + i
+  // register r of lane (n, kblk) is token 4 kblk + r, operand i column 8 n + i
   if (col >= hidden) return;
 #pragma unroll
-  for (int f = 0; f < RF; ++f)
+  for (int r = 0; r < 4; ++r) {
+    const int t = t0 + 4 * kblk + r;
+    if (t >= n_tokens) continue;
+    float v[8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = t0 + 16 * f + 4 * kblk + r;
-      if (t >= n_tokens) continue;
-      float v[8];
+    for (int i = 0; i < 8; ++i) v[i] = acc[i][r];
+    if (add) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = acc[f][i][r];
-      if (add) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[2 * i] += __uint_as_float(more[f][r][i] << 16);
-          v[2 * i + 1] += __uint_as_float(more[f][r][i] & 0xffff0000u);
-        }
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] += __uint_as_float(more[r][i] << 16);
+        v[2 * i + 1] += __uint_as_float(more[r][i] & 0xffff0000u);
       }
-      *(u32x4*)(dx + (size_t)t * hidden + col) = round_piece(v);
     }
+    *(u32x4*)(dx + (size_t)t * hidden + col) = round_piece(v);
+  }
 }
 
-// dx, fp32: 16 RF tokens x 64 columns, the experts 16 at a time; instruction s of a step has experts 4 (l / 16) + s.
-template <int RF>
+// dx, fp32: 16 tokens x 64 columns, the experts 16 at a time; instruction s of a step has experts 4 (l / 16) + s.
 __device__ __forceinline__ void router_dx_wave(const float* __restrict__ w_g, const float* __restrict__ d_logits, const float* add, int n_tokens,
                                                int n_experts, int hidden, float* dx, int t0, int slice) {
   const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
   const int col = slice * DwF32::COLS + 4 * n;
   const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
-  f32x4_t acc[RF][4];
+  f32x4_t acc[4];
 #pragma unroll
-  for (int f = 0; f < RF; ++f)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[f][i] = f32x4_t{0, 0, 0, 0};
+  for (int i = 0; i < 4; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
+  const float* row = d_logits + (size_t)min(t0 + n, n_tokens - 1) * n_experts;
   for (int e0 = 0; e0 < n_experts; e0 += 16) {
     const int e = e0 + 4 * kblk;
-    f32x4_t w[4], d[RF];
+    f32x4_t w[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
       w[s] = e + s < n_experts ? load_4(w_g + (size_t)(e + s) * hidden, col, hidden, whole_h) : f32x4_t{0, 0, 0, 0};
+    const f32x4_t d = load_4(row, e, n_experts, whole_e);
 #pragma unroll
-    for (int f = 0; f < RF; ++f) d[f] = load_4(d_logits + (size_t)min(t0 + 16 * f + n, n_tokens - 1) * n_experts, e, n_experts, whole_e);
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int f = 0; f < RF; ++f)
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[f][i] = mfma_16x16x4_f32(d[f][s], w[s][i], acc[f][i]);
+      for (int i = 0; i < 4; ++i) acc[i] = mfma_16x16x4_f32(d[s], w[s][i], acc[i]);
   }
 #pragma unroll
-  for (int f = 0; f < RF; ++f)
+  for (int r = 0; r < 4; ++r) {
+    const int t = t0 + 4 * kblk + r;
+    if (t >= n_tokens) continue;
+    f32x4_t v = {acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
+    if (add) v += load_4(add + (size_t)t * hidden, col, hidden, whole_h);
+    float* out = dx + (size_t)t * hidden;
+    if (whole_h && col < hidden) *(f32x4_t*)(out + col) = v;
+    else
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = t0 + 16 * f + 4 * kblk + r;
-      if (t >= n_tokens) continue;
-      f32x4_t v = {acc[f][0][r], acc[f][1][r], acc[f][2][r], acc[f][3][r]};
-      if (add) v += load_4(add + (size_t)t * hidden, col, hidden, whole_h);
-      float* out = dx + (size_t)t * hidden;
-      if (whole_h && col < hidden) *(f32x4_t*)(out + col) = v;
-      else
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (col + i < hidden) out[col + i] = v[i];
-    }
+      for (int i = 0; i < 4; ++i)
+        if (col + i < hidden) out[col + i] = v[i];
+  }
 }
 
 // dx of large batches: four waves per block
-template <class NUM, int RF>
-__global__ __launch_bounds__(256, RF == 1 ? 4 : 3) void router_dx_kernel(const typename NUM::T* __restrict__ w_g, const float* __restrict__ d_logits,
+template <class NUM>
+__global__ __launch_bounds__(256, 4) void router_dx_kernel(const typename NUM::T* __restrict__ w_g, const float* __restrict__ d_logits,
                                                                          const typename NUM::T* add, int n_tokens, int n_experts, int hidden,
                                                                          typename NUM::T* dx) {
-  const int t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 16 * RF;
-  if (t0 < n_tokens) router_dx_wave<RF>(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, blockIdx.y);
+  const int t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 16;
+  if (t0 < n_tokens) router_dx_wave(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, blockIdx.y);
 }
 
 // d_w_g: a block takes 16 M experts x NUM::COLS columns over some of the tokens, each of its eight waves every eighth step of
@@ -491,7 +472,7 @@ __global__ __launch_bounds__(64 * DW_WAVES, 2) void router_backward_small_kernel
     router_dw_block<NUM, 1>(x, d_logits, n_experts, hidden, b % slices, b / slices, 0, n_tokens, d_w_g, red);
   } else {
     const int i = b - dw_blocks, t0 = (i / slices * DW_WAVES + threadIdx.x / 64) * 16;
-    if (t0 < n_tokens) router_dx_wave<1>(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, i % slices);
+    if (t0 < n_tokens) router_dx_wave(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, i % slices);
   }
 }
 
@@ -544,10 +525,8 @@ static void launch_router_backward(const hmoe_layer_desc& d, const typename NUM:
     return;
   }
   if (dx) {
-    // 32 tokens per wave where that leaves every SIMD two, else 16
-    const bool two = (long)p.slices * (T / 32) >= 2048;
-    const dim3 grid((unsigned)((T + (two ? 127 : 63)) / (two ? 128 : 64)), (unsigned)p.slices);
-    hipLaunchKernelGGL((two ? &router_dx_kernel<NUM, 2> : &router_dx_kernel<NUM, 1>), grid, dim3(256), 0, s, w_g, d_logits, add, T, E, H, dx);
+    hipLaunchKernelGGL(router_dx_kernel<NUM>, dim3((unsigned)((T + 63) / 64), (unsigned)p.slices), dim3(256), 0, s, w_g, d_logits, add, T, E, H,
+                       dx);
   }
   if (d_w_g) {
     const dim3 grid((unsigned)p.slices, (unsigned)p.chunks, (unsigned)p.tiles);

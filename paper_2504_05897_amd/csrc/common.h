@@ -238,6 +238,7 @@ int launch_ffn_tiled(const FfnArgs& a);
 int launch_ffn_skinny_w4(const FfnArgs& a);
 int launch_ffn_tiled_w4(const FfnArgs& a);
 int launch_ffn_reference_i8(const FfnArgs& a);
+bool ffn_skinny_i8_takes(const hmoe_layer_desc& d, int n_rows);
 int launch_ffn_skinny_i8(const FfnArgs& a);
 int launch_ffn_tiled_i8(const FfnArgs& a);
 // codes and scales of the rows that an int8 FFN launch reads, in the call's workspace: the tokens' (sorted), then those of h

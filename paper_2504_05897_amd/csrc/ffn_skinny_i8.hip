@@ -210,6 +210,17 @@ static void launch_stage_i8(const SkinnyI8Ctx& c, int busy_max, const void* in, 
   else launch(&ffn_skinny_i8_kernel<GATEUP, 8, XF, 2, OWN>, 8);
 }
 
+// What HMOE_FFN_AUTO chooses (calls, us, these kernels / the prefill tiles): up to 16 tokens (64 experts of 3584 x 2560, top 8, 16 tokens
+// 246 / 256, 32 tokens 288 / 277; 8 of 4096 x 14336, top 2, 20 tokens 226 / 226; 64 of 2048 x 1408, top 6, 20 tokens 93 / 88; one of 3584 x
+// 20480, 16 tokens 65 / 75, 32 tokens 82 / 77), and for small layers, whose calls are a few launches' latency, while an expert's
+// rows fit a pass (16 of 1024 x 640, top 2, 77 tokens 19.0 / 21.1, 120 tokens 20.3 / 21.2, 200 tokens 24.2 / 21.9; one of 2048 x 2816, 32
+// tokens 24.6 / 29.3, 48 tokens 34.6 / 29.7).
+bool ffn_skinny_i8_takes(const hmoe_layer_desc& d, int n_rows) {
+  const int T = n_rows / d.top_k;
+  if (T <= 16) return true;
+  return 3l * d.hidden * d.ffn * d.n_experts <= (64l << 20) && (T <= 32 || n_rows <= 16 * d.n_experts);
+}
+
 int launch_ffn_skinny_i8(const FfnArgs& a) {
   const hmoe_layer_desc& d = *a.desc;
   if (d.dtype != HMOE_BF16_I8) return HMOE_ERR_UNSUPPORTED;
@@ -227,9 +238,10 @@ int launch_ffn_skinny_i8(const FfnArgs& a) {
   // costs 3 to 4 us; in a block it costs time per row, and that again in every round of blocks.  Calls, own launches / in the
   // blocks, us: 64 experts of 2048 x 1408, top 6, 1 / 4 / 8 tokens 19.0 / 16.5, 39.6 / 35.6, 61.0 / 58.7; 16 of 4096 x 1024, top 2, 8 tokens
   // 32.2 / 27.7; 8 of 4096 x 14336, top 2, 2 tokens (28672 values of h per pass) 115.0 / 112.4, 4 tokens (57344) 143.8 / 146.2, 8 tokens
-  // (3584 blocks in gate/up) 198.4 / 206.2; 64 of 3584 x 2560, top 8, 8 tokens (5120 blocks) 198.1 / 199.4.
+  // (3584 blocks in gate/up) 198.4 / 206.2; 64 of 3584 x 2560, top 8, 8 tokens (5120 blocks) 198.1 / 199.4.  Those have one or two rows per
+  // expert; one expert of 2048 x 2816, 8 tokens and rows 21 / 33.
   auto in_blocks = [&](int K, int n_out) {
-    return max_rows <= SKINNY_I8_ROWS && max_rows * K <= 32768 && (long)(n_out / TILE_N) * busy_max <= 3000;
+    return max_rows <= SKINNY_I8_ROWS && a.n_rows <= 2 * d.n_experts && max_rows * K <= 32768 && (long)(n_out / TILE_N) * busy_max <= 3000;
   };
   const bool own_x = in_blocks(d.hidden, d.ffn), own_h = in_blocks(d.ffn, d.hidden);
   const bool two = max_rows > 16;
