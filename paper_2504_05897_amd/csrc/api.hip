@@ -488,7 +488,7 @@ extern "C" int32_t hmoe_cache_get_scores(const hmoe_cache* c, double* h_out) {
 // ---- FFN dispatch ------------------------------------------------------------------------
 extern "C" size_t hmoe_ffn_workspace_bytes(const hmoe_layer_desc* desc, int32_t A) {
   if (check_desc(desc) != HMOE_OK || A < 0) return 0;
-  if (desc->dtype == HMOE_BF16_I8) return i8_work((size_t)A, (size_t)desc->hidden, (size_t)desc->ffn).total;
+  if (desc->dtype == HMOE_BF16_I8) return A > 0 ? i8_work(*desc, A).total : 0;
   const size_t elem = desc->dtype == HMOE_F32 ? 4 : 2;
   return (((size_t)A * desc->ffn * elem) + 255) & ~(size_t)255;
 }

@@ -180,18 +180,27 @@ __host__ __device__ inline size_t i8_packed_index(int n, int k, int K) {
 }
 // The smallest amax a row counts with: 127 / amax stays finite, and a row of zeros gets codes 0.
 constexpr float I8_MIN_AMAX = 0x1p-100f;
-// Workspace of an FFN call over A rows: h [A, F] fp32, the codes of the rows that the launch at hand reads ([A, H], then
-// [A, F]: the first are not needed any more when the second are written) and their scales [A].
+// Workspace of an FFN call over A rows: h [A, F] fp32, the codes of the rows that the launch at hand reads (the tokens', then
+// [A, F]: the first are not needed any more when the second are written) and their scales.  The tokens' codes are [A, H] in
+// sorted order, or one row per token and code_row [A] says which (ffn_i8.hip): the first `tokens` rows by token number, and a
+// place for every sorted row behind them.
 struct I8Work {
-  size_t codes, scales, total;  // byte offsets (h at 0)
+  size_t tokens;                                   // rows by token number
+  size_t codes, scales, code_row, owner, total;    // byte offsets (h at 0)
 };
-inline I8Work i8_work(size_t A, size_t hidden, size_t ffn) {
+inline I8Work i8_work(size_t A, size_t hidden, size_t ffn, size_t top_k) {
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   I8Work w;
-  w.codes = (A * ffn * 4 + 255) & ~(size_t)255;
-  w.scales = w.codes + ((A * (hidden > ffn ? hidden : ffn) + 255) & ~(size_t)255);
-  w.total = w.scales + ((A * 4 + 255) & ~(size_t)255);
+  w.tokens = (A + top_k - 1) / top_k;
+  const size_t rows_x = w.tokens + A;
+  w.codes = up(A * ffn * 4);
+  w.scales = w.codes + up(rows_x * hidden > A * ffn ? rows_x * hidden : A * ffn);
+  w.code_row = w.scales + up(rows_x * 4);
+  w.owner = w.code_row + up(A * 4);
+  w.total = w.owner + up(w.tokens * 4);
   return w;
 }
+inline I8Work i8_work(const hmoe_layer_desc& d, int A) { return i8_work((size_t)A, (size_t)d.hidden, (size_t)d.ffn, (size_t)d.top_k); }
 
 struct FfnArgs {
   const hmoe_layer_desc* desc = nullptr;
@@ -243,6 +252,8 @@ int launch_ffn_skinny_i8(const FfnArgs& a);
 int launch_ffn_tiled_i8(const FfnArgs& a);
 // codes and scales of the rows that an int8 FFN launch reads, in the call's workspace: the tokens' (sorted), then those of h
 void launch_quantize_x_i8(const FfnArgs& a);
+bool i8_shares_rows(const FfnArgs& a);               // whether one row of codes per token is worth it ...
+void launch_quantize_shared_x_i8(const FfnArgs& a);  // ... which this makes, with code_row
 void launch_quantize_h_i8(const FfnArgs& a);
 
 }  // namespace hmoe

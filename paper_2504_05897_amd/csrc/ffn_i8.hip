@@ -40,14 +40,10 @@ __device__ __forceinline__ bool row_takes_part(const I8Ctx& c, int p) {
   return c.active.test(e) && c.slot_of[e] >= 0;
 }
 
-// codes[p] and scales[p] of sorted row p of `in` (through the row map if there is one), whose values stay in registers between
-// the row's maximum and its codes.  Rows of up to 64 * 8 * HELD values: a wavefront each, four per block and no barrier.
+// Codes and scale of a row by a wavefront, which holds its values in registers between their maximum and the codes.
 template <class T, int HELD>
-__global__ __launch_bounds__(256) void quantize_rows_wave_kernel(I8Ctx c, const T* __restrict__ in, int n_rows, int K,
-                                                                 int8_t* __restrict__ codes, float* __restrict__ scales) {
-  const int p = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), lane = threadIdx.x % 64;
-  if (p >= n_rows || !row_takes_part(c, p)) return;
-  const T* row = in + (size_t)mapped_row(c.row_map, c.map_div, p) * K;
+__device__ __forceinline__ void quantize_row_wave(const T* __restrict__ row, int K, int8_t* __restrict__ out, float* __restrict__ scale) {
+  const int lane = threadIdx.x % 64;
   float v[HELD][8];
   uint32_t m = 0;
 #pragma unroll
@@ -62,13 +58,22 @@ __global__ __launch_bounds__(256) void quantize_rows_wave_kernel(I8Ctx c, const 
   for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
   const RowQuant q = row_quant(m);
   constexpr bool EXACT = sizeof(T) == 2;
-  int8_t* out = codes + (size_t)p * K;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     const int k = 8 * (i * 64 + lane);
     if (k < K) *(uint2*)(out + k) = codes_of<EXACT>(v[i], q);
   }
-  if (lane == 0) scales[p] = q.scale;
+  if (lane == 0) *scale = q.scale;
+}
+
+// codes[p] and scales[p] of sorted row p of `in` (through the row map if there is one).  Rows of up to 64 * 8 * HELD values: a
+// wavefront each, four per block and no barrier.
+template <class T, int HELD>
+__global__ __launch_bounds__(256) void quantize_rows_wave_kernel(I8Ctx c, const T* __restrict__ in, int n_rows, int K,
+                                                                 int8_t* __restrict__ codes, float* __restrict__ scales) {
+  const int p = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
+  if (p >= n_rows || !row_takes_part(c, p)) return;
+  quantize_row_wave<T, HELD>(in + (size_t)mapped_row(c.row_map, c.map_div, p) * K, K, codes + (size_t)p * K, scales + p);
 }
 
 // Longer rows: a block of 1024 threads each.  What is beyond 16 values per thread is read twice.
@@ -94,6 +99,45 @@ static void launch_quantize(const I8Ctx& c, int n_rows, const T* in, int K, int8
   else if (K <= 2048) waves(&quantize_rows_wave_kernel<T, 4>);
   else if (K <= 4096) waves(&quantize_rows_wave_kernel<T, 8>);
   else hipLaunchKernelGGL(quantize_rows_block_kernel<T>, dim3((unsigned)n_rows), dim3(1024), 0, s, c, in, K, codes, scales);
+}
+
+// ---- one row of codes per token ---------------------------------------------------------------
+// A batch with a row map reads every token top_k times.  Its codes once per token are a K-th of the traffic (16384 tokens of
+// 2048, top 6: SEE_BELOW), and the tiles find them through code_row as they find bfloat16 rows through the row map.  Only rows
+// that the map names are read, whatever it names: a first launch notes for each token one sorted row that names it, and a
+// second quantises the tokens whose note is true (memory that nothing was noted in may hold anything).  Tokens past the
+// expected number, as calls over some of the assignments may name, get a row per sorted row behind the others.
+__global__ __launch_bounds__(256) void note_tokens_kernel(I8Ctx c, int n_tokens, int32_t* __restrict__ code_row, int32_t* __restrict__ owner) {
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p >= c.offsets[c.n_experts]) return;
+  const int t = c.row_map[p] / c.map_div;
+  const bool by_token = (unsigned)t < (unsigned)n_tokens;
+  code_row[p] = by_token ? t : n_tokens + p;
+  if (by_token) __hip_atomic_store(owner + t, p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // (one of them, whichever)
+}
+
+constexpr int FAR_BLOCKS = 64;  // in front: they look through the row map for tokens past the expected number
+template <int HELD>
+__global__ __launch_bounds__(256) void quantize_tokens_kernel(I8Ctx c, const bf16_t* __restrict__ x, int n_tokens, const int32_t* __restrict__ owner,
+                                                              int8_t* __restrict__ codes, float* __restrict__ scales) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, H = c.hidden;
+  const int n = c.offsets[c.n_experts];
+  if (blockIdx.x >= FAR_BLOCKS) {
+    const int t = (blockIdx.x - FAR_BLOCKS) * 4 + wave;
+    if (t >= n_tokens) return;
+    const int p = owner[t];
+    if ((unsigned)p >= (unsigned)n || c.row_map[p] / c.map_div != t) return;
+    quantize_row_wave<bf16_t, HELD>(x + (size_t)t * H, H, codes + (size_t)t * H, scales + t);
+    return;
+  }
+  for (int p0 = (blockIdx.x * 4 + wave) * 64; p0 < n; p0 += FAR_BLOCKS * 256) {
+    const int t = p0 + lane < n ? c.row_map[p0 + lane] / c.map_div : 0;
+    for (uint64_t far = __ballot(t >= n_tokens); far; far &= far - 1) {
+      const int l = __ffsll((long long)far) - 1;
+      const size_t to = (size_t)n_tokens + p0 + l;
+      quantize_row_wave<bf16_t, HELD>(x + (size_t)__builtin_amdgcn_readlane(t, l) * H, H, codes + to * H, scales + to);
+    }
+  }
 }
 
 // ---- the reference path: one wavefront per output element ------------------------------------
@@ -161,15 +205,35 @@ static I8Ctx i8_ctx(const FfnArgs& a) {
                a.row_map, a.map_div};
 }
 void launch_quantize_x_i8(const FfnArgs& a) {
-  const I8Work w = i8_work((size_t)a.n_rows, (size_t)a.desc->hidden, (size_t)a.desc->ffn);
+  const I8Work w = i8_work(*a.desc, a.n_rows);
   launch_quantize(i8_ctx(a), a.n_rows, (const bf16_t*)a.x_perm, a.desc->hidden, (int8_t*)a.h + w.codes, (float*)((char*)a.h + w.scales),
                   a.stream);
 }
 void launch_quantize_h_i8(const FfnArgs& a) {
-  const I8Work w = i8_work((size_t)a.n_rows, (size_t)a.desc->hidden, (size_t)a.desc->ffn);
+  const I8Work w = i8_work(*a.desc, a.n_rows);
   I8Ctx c = i8_ctx(a);
   c.row_map = nullptr;  // h is in sorted order
   launch_quantize(c, a.n_rows, (const float*)a.h, a.desc->ffn, (int8_t*)a.h + w.codes, (float*)((char*)a.h + w.scales), a.stream);
+}
+
+bool i8_shares_rows(const FfnArgs& a) {
+  // (rows of more than 4096 values are quantised by whole blocks; a few MiB of codes are not worth a launch)
+  return a.row_map && a.map_div > 1 && a.desc->hidden <= 4096 && (size_t)a.n_rows * a.desc->hidden >= (size_t)8 << 20;
+}
+void launch_quantize_shared_x_i8(const FfnArgs& a) {
+  const I8Ctx c = i8_ctx(a);
+  const I8Work w = i8_work(*a.desc, a.n_rows);
+  int32_t* code_row = (int32_t*)((char*)a.h + w.code_row);
+  int32_t* owner = (int32_t*)((char*)a.h + w.owner);
+  const int T = (int)w.tokens, H = a.desc->hidden;
+  hipLaunchKernelGGL(note_tokens_kernel, dim3((unsigned)((a.n_rows + 255l) / 256)), dim3(256), 0, a.stream, c, T, code_row, owner);
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(FAR_BLOCKS + (T + 3l) / 4)), dim3(256), 0, a.stream, c, (const bf16_t*)a.x_perm, T, owner,
+                       (int8_t*)a.h + w.codes, (float*)((char*)a.h + w.scales));
+  };
+  if (H <= 1024) launch(&quantize_tokens_kernel<2>);
+  else if (H <= 2048) launch(&quantize_tokens_kernel<4>);
+  else launch(&quantize_tokens_kernel<8>);
 }
 
 int launch_ffn_reference_i8(const FfnArgs& a) {
@@ -177,7 +241,7 @@ int launch_ffn_reference_i8(const FfnArgs& a) {
   if (a.n_rows == 0) return HMOE_OK;
   if ((d.ffn + 3) / 4 > 65535 || (d.hidden + 3) / 4 > 65535) return HMOE_ERR_UNSUPPORTED;
   const I8Ctx c = i8_ctx(a);
-  const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
+  const I8Work w = i8_work(d, a.n_rows);
   const int8_t* codes = (const int8_t*)a.h + w.codes;
   const float* scales = (const float*)((const char*)a.h + w.scales);
   launch_quantize_x_i8(a);

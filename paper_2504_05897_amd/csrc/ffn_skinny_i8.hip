@@ -231,7 +231,7 @@ int launch_ffn_skinny_i8(const FfnArgs& a) {
   SkinnyI8Ctx c{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, d.n_experts, d.hidden, d.ffn, (uint32_t)x_bytes, 0, a.row_map, a.map_div};
   const int busy_max = std::min(d.n_experts, a.n_rows);          // every busy expert has at least one row
   const int max_rows = std::max(1, a.n_rows / d.top_k);          // a token names an expert at most once
-  const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
+  const I8Work w = i8_work(d, a.n_rows);
   const int8_t* codes = (const int8_t*)a.h + w.codes;
   const float* scales = (const float*)((const char*)a.h + w.scales);
   // Rows quantised by the blocks that read them (max_rows of them per pass, in LDS) or by a launch of its own.  The launch

@@ -35,7 +35,7 @@ __device__ __forceinline__ void run_tile_i8(const TiledCtx& c, const bf16_t* __r
     col_scales[j] = scales[(TILE::GATEUP ? g / 2 : g) * TILE_N + col];
   }
   typename TILE::Sums sums;
-  TILE::scale_sums(loc, row_scales, col_scales, acc, lds, sums);
+  TILE::scale_sums(c, loc, row_scales, col_scales, acc, lds, sums);
   if constexpr (TILE::GATEUP && TILE::FN == 2) TILE::epilogue_h_f32(c, out, loc, sums);
   else if constexpr (TILE::GATEUP) TILE::epilogue_pairs(c, out, loc, sums, lds);
   else if constexpr (TILE::FN == 2) TILE::epilogue_lines_down(c, out, loc, sums, lds);
@@ -94,7 +94,7 @@ struct WalkI8Lds {
   int rows[WALK_ROWS * 256];
 };
 
-// the sorted row whose scale this thread copies: row `tid` of the tile
+// the sorted row whose scale this thread copies: that of row `tid` of the tile
 __device__ __forceinline__ int walk_scale_row(const TiledCtx& c, const TileLoc& loc, int tid) {
   return loc.row_first + min(loc.m0 + tid, loc.m_rows - 1);
 }
@@ -301,7 +301,7 @@ int launch_ffn_tiled_i8(const FfnArgs& a) {
   if (d.dtype != HMOE_BF16_I8) return HMOE_ERR_UNSUPPORTED;
   if (a.n_rows == 0) return HMOE_OK;
   TiledCtx c{a.offsets, a.slot_of, a.slots, a.slot_bytes, a.active, d.n_experts, d.hidden, d.ffn, 0, 0, nullptr, 1};
-  const I8Work w = i8_work((size_t)a.n_rows, (size_t)d.hidden, (size_t)d.ffn);
+  const I8Work w = i8_work(d, a.n_rows);
   const bf16_t* codes = (const bf16_t*)((const char*)a.h + w.codes);
   const float* scales = (const float*)((const char*)a.h + w.scales);
   I8Choice gate_up = choose_i8(d, a.n_rows, true), down = choose_i8(d, a.n_rows, false);
@@ -314,7 +314,12 @@ int launch_ffn_tiled_i8(const FfnArgs& a) {
     gate_up = forced(env[0], d.hidden, gate_up);
     if (env[0]) down = forced(env[1], d.ffn, down);
   }
-  launch_quantize_x_i8(a);
+  if (i8_shares_rows(a)) {
+    launch_quantize_shared_x_i8(a);
+    c.row_map = (const int32_t*)((const char*)a.h + w.code_row);
+  } else {
+    launch_quantize_x_i8(a);
+  }
   probe_before(a.stream);
   launch_stage_i8<true>(c, gate_up.shape, gate_up.nt, a.n_rows, codes, scales, (float*)a.h, a.stream);
   probe_after(a.stream);

@@ -609,16 +609,20 @@ struct StreamTile {
       if (m < m_rows && f < n_out) *(u32x4*)(out + (size_t)(row_first + m) * n_out + f) = v;
     }
   }
-  // Integer sums times the scales of their rows and columns.  row_scales: per sorted row; they reach the lanes through LDS, four
+  // Integer sums times the scales of their rows and columns.  row_scales: per input row; they reach the lanes through LDS, four
   // consecutive rows at a time (a lane's 16 sums per fragment are four runs of four rows).  col_scales: of the lane's column of
   // each group.
-  static __device__ __forceinline__ void scale_sums(const TileLoc& loc, const float* __restrict__ row_scales,
+  static __device__ __forceinline__ void scale_sums(const TiledCtx& c, const TileLoc& loc, const float* __restrict__ row_scales,
                                                     const float (&col_scales)[FN], const Acc& acc, u32x4* lds, Sums& sums) {
     const int tid = threadIdx.x, half = tid % 64 / 32;
     const int m0 = loc.mt * MSTRIDE;
     float* staged = (float*)lds;
     block_barrier();  // every wave has read its last activation fragments
-    if (tid < FM * 32) staged[tid] = row_scales[loc.row_first + (m0 + tid < loc.m_rows ? m0 + tid : loc.m_rows - 1)];
+    if (tid < FM * 32) {
+      int row = loc.row_first + (m0 + tid < loc.m_rows ? m0 + tid : loc.m_rows - 1);
+      if (GATEUP && c.row_map) row = div_by_map(c, c.row_map[row]);
+      staged[tid] = row_scales[row];
+    }
     static_assert(FM * 32 <= THREADS, "a thread per row");
     __syncthreads();
 #pragma unroll

@@ -342,3 +342,35 @@ def test_walking_blocks_with_many_tiles_each(hm, monkeypatch):
     for _ in range(3):
         assert torch.equal(grouped(*args).view(torch.int16), want.view(torch.int16))
     layer.close()
+
+
+@pytest.mark.parametrize("T,far", [(4500, False), (6500, True)])
+def test_codes_once_per_token(hm, T, far):
+    """A batch large enough for one row of codes per token.  The same bits as over the gathered rows, and for a call over some of
+    the assignments, whose permutation names tokens past A / K, too."""
+    say("i8 codes per token", T, far)
+    H, E, K = 1024, 7, 2
+    d, experts, layer = make(hm, H, 896, E, K, 13, distinct=2)
+    rng = np.random.default_rng(17)
+    idx = np.argsort(rng.standard_normal((T, E)), axis=1)[:, :K]
+    perm = np.argsort(idx.ravel(), kind="stable").astype(np.int32)
+    keep = np.ones(T * K, bool)
+    if far:                                          # the assignments of two experts are left out, and some tokens altogether
+        keep = ~np.isin(idx.ravel()[perm], [2, 3]) & (perm // K % 97 != 0)
+    perm = perm[keep]
+    offsets = offsets_of(np.bincount(idx.ravel()[perm], minlength=E))
+    A = len(perm)
+    assert A * H >= 8 << 20 and (not far or (perm // K >= -(-A // K)).any())
+    # (tokens that the permutation does not name hold NaN: nothing may come of them)
+    x = np.full((T, H), 0x7fc0, np.uint16)
+    named = np.unique(perm // K)
+    x[named] = rows_of(12, len(named), H)
+    x, perm, offsets = to_device(x), to_device(perm), to_device(offsets)
+    ws, n = workspace(hm, d, A)
+    a, b = (torch.full((A, H), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    for seed in range(2):                            # the second time over a workspace full of the first one's notes
+        hm.hmoe_expert_ffn_grouped_gather(d, layer.cache, x, perm, offsets, A, None, a, ws, n, TILED)
+        hm.hmoe_expert_ffn_grouped(d, layer.cache, x[(perm // K).long()].contiguous(), offsets, A, None, b, torch.empty_like(ws), n, TILED)
+        torch.cuda.synchronize()
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and a.isfinite().all() and (ws[n:] == 0x5a).all()
+    layer.close()
