@@ -74,7 +74,7 @@ class LayerDesc(ctypes.Structure):
 
     def __repr__(self):
         return "LayerDesc(H=%d, F=%d, E=%d, K=%d, S=%d, %s)" % (
-            self.hidden, self.ffn, self.n_experts, self.top_k, self.n_slots, "bf16" if self.dtype else "f32")
+            self.hidden, self.ffn, self.n_experts, self.top_k, self.n_slots, {0: "f32", 3: "i8"}.get(self.dtype, "bf16"))
 
 
 class LayerCall(ctypes.Structure):
@@ -733,6 +733,35 @@ class MoELayer:
                                         self.o_shared, self.shared_ws, self.shared_ws_bytes, path)
         hmoe_combine(d, self.o_perm, self.inv_perm, self.topk_w, o_shared, T, self.y)
         return self.y[:T]
+
+    # -- training the router ----------------------------------------------------------------
+    def router_gradient(self, x: torch.Tensor, dy: torch.Tensor, dx: Optional[torch.Tensor] = None):
+        """Gradient of the last forward pass on ``x`` [T, H] with respect to the router, from ``dy`` = dL/dy [T, H] (layer dtype),
+        over experts that stay as they are: the weighted sum's, the gates' and the router product's gradients in a row.
+
+        Returns (d_w_router [E, H] fp32, or None where the layer has no router; d_logits [T, E] fp32), views of internal buffers,
+        valid until the next call.  ``dx`` [T, H] (layer dtype), if given, has the router's part of dL/dx added to it."""
+        d = self.desc
+        T = x.shape[0]
+        assert T <= self.max_tokens and x.dtype == self.dt and x.is_contiguous()
+        assert dy.shape == x.shape and dy.dtype == self.dt and dy.is_contiguous()
+        assert dx is None or (dx.shape == x.shape and dx.dtype == self.dt and dx.is_contiguous())
+        assert dx is None or self.w_router is not None, "a layer without a router has no input gradient through it"
+        if getattr(self, "_grad_tokens", 0) < self.max_tokens:
+            self._grad_tokens = self.max_tokens
+            f32 = dict(dtype=torch.float32, device=self.dev)
+            self._d_topk_w = torch.empty(self._grad_tokens, d.top_k, **f32)
+            self._d_logits = torch.empty(self._grad_tokens, d.n_experts, **f32)
+            self._d_w_router = torch.empty(d.n_experts, d.hidden, **f32)
+            self._grad_ws_bytes = hmoe_router_backward_workspace_bytes(d, self._grad_tokens)
+            self._grad_ws = torch.empty(self._grad_ws_bytes, dtype=torch.uint8, device=self.dev)
+        d_w = None
+        hmoe_combine_backward(d, dy, self.o_perm, self.inv_perm, None, T, None, self._d_topk_w)
+        hmoe_route_backward(d, self.topk_idx, self.topk_w, self._d_topk_w, T, self._d_logits)
+        if self.w_router is not None:
+            d_w = self._d_w_router
+            hmoe_router_backward(d, x, self.w_router, self._d_logits, T, dx, dx, d_w, self._grad_ws, self._grad_ws_bytes)
+        return d_w, self._d_logits[:T]
 
     # -- score-aware replacement (Section IV-D) -------------------------------------------
     def set_policy(self, policy: int, alpha: float = 0.5):

@@ -103,7 +103,7 @@ static void launch_quantize(const I8Ctx& c, int n_rows, const T* in, int K, int8
 
 // ---- one row of codes per token ---------------------------------------------------------------
 // A batch with a row map reads every token top_k times.  Its codes once per token are a K-th of the traffic (16384 tokens of
-// 2048, top 6: SEE_BELOW), and the tiles find them through code_row as they find bfloat16 rows through the row map.  Only rows
+// 2048, top 6: 100 -> 34 us), and the tiles find them through code_row as they find bfloat16 rows through the row map.  Only rows
 // that the map names are read, whatever it names: a first launch notes for each token one sorted row that names it, and a
 // second quantises the tokens whose note is true (memory that nothing was noted in may hold anything).  Tokens past the
 // expected number, as calls over some of the assignments may name, get a row per sorted row behind the others.

@@ -244,3 +244,90 @@ def test_gradients_in_a_graph(hm, dtype):
         want = chain(ws[1])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
+
+
+@pytest.mark.parametrize("dtype,T", [("i8", 5), ("i8", 300), ("bf16", 40), ("f32", 9)])
+def test_router_gradient_of_a_layer(hm, dtype, T):
+    """A forward pass and the gradient of 1/2 |y - target|^2 with respect to the router, experts held: against the oracle's chain
+    over the pass's own choice and expert outputs."""
+    say("router gradient", dtype, T)
+    bf16 = dtype != "f32"
+    shape = wl.small_shape(dtype=wl.BF16 if bf16 else wl.F32, hidden=256, ffn=128, n_experts=8, top_k=2, shared_ffn=(128,), x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 7, T)
+    kind = {"f32": hm.HMOE_F32, "bf16": hm.HMOE_BF16, "i8": hm.HMOE_BF16_I8}[dtype]
+    layer = hm.MoELayer(hm.make_desc(256, 128, 8, 2, 8, kind), lay.experts, lay.shared, lay.w_router, max_tokens=T + 3)
+    x = to_device(lay.x)
+    y = layer.forward(x)
+    target = torch.randn(T, 256, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).to(y.dtype)
+    dy = (y - target).contiguous()
+    seen = torch.randn(T, 256, device=DEV, generator=torch.Generator(device=DEV).manual_seed(2)).to(y.dtype)
+    dx = seen.clone()
+    d_w, d_logits = layer.router_gradient(x, dy, dx)
+    torch.cuda.synchronize()
+    f = lambda t: t.double().cpu().numpy()
+    idx, w, inv = layer.topk_idx[:T].cpu().numpy(), f(layer.topk_w[:T]), layer.inv_perm[:2 * T].cpu().numpy()
+    o = f(layer.o_perm[:2 * T])
+    _, d_topk = go.combine_backward(f(dy), o, inv, w)
+    ref_l = go.route_backward(idx, w, d_topk, 8)
+    ref_dx, ref_w = go.router_backward(f(x), wl.as_f64(lay.w_router), ref_l, f(seen))
+    # d_topk_w: 256 products; |d_logits| <= 2 w max |d_topk_w|
+    mags = np.stack([(np.abs(f(dy)[t]) * np.abs(o[inv[2 * t:2 * t + 2]])).sum(1) for t in range(T)]).max(1, keepdims=True)
+    slack = 2 * (256 + 8) * U * mags * (ref_l != 0)
+    assert (np.abs(f(d_logits) - ref_l) <= slack).all()
+    xa, wa = np.abs(f(x)), np.abs(wl.as_f64(lay.w_router))
+    slack_w = slack.T @ xa + (T + 2) * U * (np.abs(ref_l).T @ xa)
+    assert (np.abs(f(d_w) - ref_w) <= slack_w).all()
+    slack_x = slack @ wa + ((8 + 2) * U + 2.0 ** -17) * (np.abs(ref_l) @ wa + np.abs(f(seen)))
+    assert (np.abs(f(dx) - ref_dx) <= slack_x + (2.0 ** -8 if bf16 else U) * (np.abs(ref_dx) + slack_x)).all()
+    # a smaller batch of the same layer, and the layer without an input gradient asked for
+    layer.forward(x[:1].contiguous())
+    d_w, d_logits = layer.router_gradient(x[:1].contiguous(), dy[:1].contiguous())
+    torch.cuda.synchronize()
+    assert d_logits.shape == (1, 8) and torch.isfinite(d_w).all()
+    layer.close()
+
+
+def test_router_gradient_captured_with_the_forward_pass(hm):
+    """A training step of the router in a graph, replayed as the weights change: int8 experts, gradient, and the eager step's bits."""
+    say("router training step in a graph")
+    T = 130
+    shape = wl.small_shape(dtype=wl.BF16, hidden=256, ffn=128, n_experts=8, top_k=2, x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 9, T)
+    a, b = (hm.MoELayer(hm.make_desc(256, 128, 8, 2, 8, hm.HMOE_BF16_I8), lay.experts, (), lay.w_router, max_tokens=T) for _ in range(2))
+    x = to_device(lay.x)
+    dy = torch.randn(T, 256, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3)).bfloat16()
+
+    def step(layer):
+        layer.forward(x)
+        return layer.router_gradient(x, dy)
+
+    step(a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got_w, got_l = step(a)
+    for seed in range(3):
+        w = a.w_router + 0.01 * torch.randn(8, 256, device=DEV, generator=torch.Generator(device=DEV).manual_seed(seed)).bfloat16()
+        a.w_router.copy_(w)
+        b.w_router.copy_(w)
+        graph.replay()
+        torch.cuda.synchronize()
+        want_w, want_l = step(b)
+        torch.cuda.synchronize()
+        assert torch.equal(got_w, want_w) and torch.equal(got_l, want_l), seed
+    a.close()
+    b.close()
+
+
+def test_layer_without_a_router(hm):
+    say("router gradient, logits from outside")
+    shape = wl.small_shape(dtype=wl.BF16, hidden=256, ffn=128, n_experts=8, top_k=2)
+    lay = wl.make_layer(shape, 3, 6)
+    layer = hm.MoELayer(hm.make_desc(256, 128, 8, 2, 8, hm.HMOE_BF16_I8), lay.experts, (), None, max_tokens=6)
+    x, logits = to_device(lay.x), torch.randn(6, 8, device=DEV)
+    y = layer.forward(x, logits)
+    d_w, d_logits = layer.router_gradient(x, y.clone())
+    torch.cuda.synchronize()
+    assert d_w is None and d_logits.shape == (6, 8) and torch.isfinite(d_logits).all()
+    assert (d_logits.sum(1).abs() <= 1e-5 * d_logits.abs().sum(1) + 1e-12).all()      # softmax does not see a shift of all logits
+    layer.close()
