@@ -157,12 +157,15 @@ __device__ __forceinline__ u32x4 take_piece(float (&v)[8]) {
 __device__ __forceinline__ u32x4 round_piece(const float (&v)[8]) {
   return u32x4{f32_to_bf16_pair(v[0], v[1]), f32_to_bf16_pair(v[2], v[3]), f32_to_bf16_pair(v[4], v[5]), f32_to_bf16_pair(v[6], v[7])};
 }
-// values i0 .. i0 + 4 of a row of n (0 past its end); whole: rows and their pieces are 16-byte aligned
-__device__ __forceinline__ f32x4_t load_4(const float* row, int i0, int n, bool whole) {
-  if (whole) return i0 < n ? *(const f32x4_t*)(row + i0) : f32x4_t{0, 0, 0, 0};
+// Values i0 .. i0 + 4 of a row of n; past its end other values of the row, whose results are not stored or meet zeros.  (Always
+// loaded: a load behind a condition makes the wave wait for those before it.)  WHOLE: n is a multiple of 4, and rows 16-byte
+// aligned.
+template <bool WHOLE>
+__device__ __forceinline__ f32x4_t load_4(const float* row, int i0, int n) {
+  if (WHOLE) return *(const f32x4_t*)(row + min(i0, n - 4));
   f32x4_t v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = i0 + i < n ? row[i0 + i] : 0.0f;
+  for (int i = 0; i < 4; ++i) v[i] = row[min(i0 + i, n - 1)];
   return v;
 }
 __device__ __forceinline__ f32x4_t mfma_16x16x4_f32(float a, float b, f32x4_t c) {
@@ -181,18 +184,18 @@ struct DwF32 {
 
 // dx, bfloat16: a wave takes 16 tokens from t0 x 128 columns (slice) and goes through the experts 32 at a time.  (32 tokens for
 // each load of W_g: 69 against 68 us for gates and router of 16384 tokens; the more waves that fit hide more.)
+template <bool WHOLE>
 __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits, const bf16_t* add,
                                                int n_tokens, int n_experts, int hidden, bf16_t* dx, int t0, int slice) {
   const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
   const int col = slice * DwBf16::COLS + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
-  const bool whole = n_experts % 4 == 0;
   f32x4_t acc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
   u32x4 more[4];  // `add`, on its way while the experts are multiplied
   if (add) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) more[r] = *(const u32x4*)(add + (size_t)min(t0 + 4 * kblk + r, n_tokens - 1) * hidden + col_at);
+    for (int r = 0; r < 4; ++r) more[r] = __builtin_nontemporal_load((const u32x4*)(add + (size_t)min(t0 + 4 * kblk + r, n_tokens - 1) * hidden + col_at));
   }
   const float* row = d_logits + (size_t)min(t0 + n, n_tokens - 1) * n_experts;
   for (int e0 = 0; e0 < n_experts; e0 += 32) {
@@ -200,10 +203,10 @@ __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, c
     u32x4 w[8], op[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) w[k] = *(const u32x4*)(w_g + (size_t)min(e + k, n_experts - 1) * hidden + col_at);
-    const f32x4_t d0 = load_4(row, e, n_experts, whole), d1 = load_4(row, e + 4, n_experts, whole);
+    const f32x4_t d0 = load_4<WHOLE>(row, e, n_experts), d1 = load_4<WHOLE>(row, e + 4, n_experts);
     if (e0 + 32 > n_experts) {  // uniform
 #pragma unroll
-      for (int k = 0; k < 8; ++k)  // (a row of W_g past the last would meet zeros, but may hold an infinity)
+      for (int k = 0; k < 8; ++k)  // (meets a value of the token's own row: if that is infinite, so is the token's result already)
         if (e + k >= n_experts) w[k] = u32x4{0, 0, 0, 0};
     }
 #pragma unroll
@@ -234,16 +237,16 @@ __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, c
         v[2 * i + 1] += __uint_as_float(more[r][i] & 0xffff0000u);
       }
     }
-    *(u32x4*)(dx + (size_t)t * hidden + col) = round_piece(v);
+    __builtin_nontemporal_store(round_piece(v), (u32x4*)(dx + (size_t)t * hidden + col));
   }
 }
 
 // dx, fp32: 16 tokens x 64 columns, the experts 16 at a time; instruction s of a step has experts 4 (l / 16) + s.
+template <bool WHOLE>
 __device__ __forceinline__ void router_dx_wave(const float* __restrict__ w_g, const float* __restrict__ d_logits, const float* add, int n_tokens,
                                                int n_experts, int hidden, float* dx, int t0, int slice) {
   const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
   const int col = slice * DwF32::COLS + 4 * n;
-  const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
   f32x4_t acc[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
@@ -253,8 +256,13 @@ __device__ __forceinline__ void router_dx_wave(const float* __restrict__ w_g, co
     f32x4_t w[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      w[s] = e + s < n_experts ? load_4(w_g + (size_t)(e + s) * hidden, col, hidden, whole_h) : f32x4_t{0, 0, 0, 0};
-    const f32x4_t d = load_4(row, e, n_experts, whole_e);
+      w[s] = load_4<WHOLE>(w_g + (size_t)min(e + s, n_experts - 1) * hidden, col, hidden);
+    const f32x4_t d = load_4<WHOLE>(row, e, n_experts);
+    if (e0 + 16 > n_experts) {  // uniform
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (e + s >= n_experts) w[s] = f32x4_t{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -265,54 +273,56 @@ __device__ __forceinline__ void router_dx_wave(const float* __restrict__ w_g, co
     const int t = t0 + 4 * kblk + r;
     if (t >= n_tokens) continue;
     f32x4_t v = {acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
-    if (add) v += load_4(add + (size_t)t * hidden, col, hidden, whole_h);
+    if (add) v += load_4<WHOLE>(add + (size_t)t * hidden, col, hidden);
     float* out = dx + (size_t)t * hidden;
-    if (whole_h && col < hidden) *(f32x4_t*)(out + col) = v;
-    else
+    if (WHOLE) {
+      if (col < hidden) *(f32x4_t*)(out + col) = v;
+    } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (col + i < hidden) out[col + i] = v[i];
+    }
   }
 }
 
 // dx of large batches: four waves per block
-template <class NUM>
+template <class NUM, bool WHOLE>
 __global__ __launch_bounds__(256, 4) void router_dx_kernel(const typename NUM::T* __restrict__ w_g, const float* __restrict__ d_logits,
                                                                          const typename NUM::T* add, int n_tokens, int n_experts, int hidden,
                                                                          typename NUM::T* dx) {
   const int t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 16;
-  if (t0 < n_tokens) router_dx_wave(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, blockIdx.y);
+  if (t0 < n_tokens) router_dx_wave<WHOLE>(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, blockIdx.y);
 }
 
-// d_w_g: a block takes 16 M experts x NUM::COLS columns over some of the tokens, each of its eight waves every eighth step of
-// STEP tokens.  The waves' sums meet in LDS, the blocks' of several chunks of the tokens in router_dw_sum_kernel, all in a
+// d_w_g: a block takes 16 M experts x NUM::COLS columns over some of the tokens, its waves a step of STEP tokens each
+// in turn.  The waves' sums meet in LDS, the blocks' of several chunks of the tokens in router_dw_sum_kernel, all in a
 // fixed order.  M = 4: a step's x serves 64 experts; M = 1: four times the blocks, for batches that make few.
 //
 // The operands of a step.  Tokens past the end are cleared where they are multiplied, in the step that has some: behind the
 // loads it would be a wait for them.  Operand m of lane n has expert e + m, e = e0 + M n.
-template <class NUM, int M>
+template <class NUM, int M, bool WHOLE>
 struct DwStep;
-template <int M>
-__device__ __forceinline__ void load_logits(float (&v)[M], const float* row, int e, int n_experts, bool whole) {
+template <int M, bool WHOLE>
+__device__ __forceinline__ void load_logits(float (&v)[M], const float* row, int e, int n_experts) {
   if constexpr (M == 4) {
-    const f32x4_t q = load_4(row, e, n_experts, whole);
+    const f32x4_t q = load_4<WHOLE>(row, e, n_experts);
 #pragma unroll
     for (int m = 0; m < 4; ++m) v[m] = q[m];
   } else {
-    v[0] = e < n_experts ? row[e] : 0.0f;
+    v[0] = row[min(e, n_experts - 1)];
   }
 }
-template <int M>
-struct DwStep<DwBf16, M> {
+template <int M, bool WHOLE>
+struct DwStep<DwBf16, M, WHOLE> {
   u32x4 x[8];
   float d[8][M];
   __device__ __forceinline__ void load(const bf16_t* __restrict__ x_in, const float* __restrict__ d_logits, int t0, int t_end, int col_at,
-                                       int e, int n_experts, int hidden, bool whole_e, bool, int kblk) {
+                                       int e, int n_experts, int hidden, int kblk) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int at = min(t0 + 8 * kblk + k, t_end - 1);
       x[k] = *(const u32x4*)(x_in + (size_t)at * hidden + col_at);
-      load_logits<M>(d[k], d_logits + (size_t)at * n_experts, e, n_experts, whole_e);
+      load_logits<M, WHOLE>(d[k], d_logits + (size_t)at * n_experts, e, n_experts);
     }
   }
   // left: tokens from t0 to the end
@@ -344,17 +354,17 @@ struct DwStep<DwBf16, M> {
     }
   }
 };
-template <int M>
-struct DwStep<DwF32, M> {
+template <int M, bool WHOLE>
+struct DwStep<DwF32, M, WHOLE> {
   f32x4_t x[4];
   float d[4][M];
   __device__ __forceinline__ void load(const float* __restrict__ x_in, const float* __restrict__ d_logits, int t0, int t_end, int col_at, int e,
-                                       int n_experts, int hidden, bool whole_e, bool whole_h, int kblk) {
+                                       int n_experts, int hidden, int kblk) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int at = min(t0 + 4 * k + kblk, t_end - 1);
-      x[k] = load_4(x_in + (size_t)at * hidden, col_at, hidden, whole_h);
-      load_logits<M>(d[k], d_logits + (size_t)at * n_experts, e, n_experts, whole_e);
+      x[k] = load_4<WHOLE>(x_in + (size_t)at * hidden, col_at, hidden);
+      load_logits<M, WHOLE>(d[k], d_logits + (size_t)at * n_experts, e, n_experts);
     }
   }
   __device__ __forceinline__ void multiply(f32x4_t (&acc)[M][4], int left, int kblk) {
@@ -376,43 +386,46 @@ struct DwStep<DwF32, M> {
   }
 };
 
-constexpr int DW_WAVES = 8;  // two per SIMD: one multiplies while the other's step is on its way
-template <class NUM>
-using DwRed = float[DW_WAVES][NUM::PIECE * 4][64];
+template <class NUM, int WAVES>
+using DwRed = float[WAVES][NUM::PIECE * 4][64];
 
 // experts 16 M tile .., columns of `slice`, tokens t_begin .. t_end -> out [E, H]
-template <class NUM, int M>
+// AHEAD steps per wave are on their way while one is multiplied.
+template <class NUM, int M, int WAVES, int AHEAD, bool WHOLE>
 __device__ __forceinline__ void router_dw_block(const typename NUM::T* __restrict__ x, const float* __restrict__ d_logits, int n_experts,
                                                 int hidden, int slice, int tile, int t_begin, int t_end, float* __restrict__ out,
-                                                DwRed<NUM>& red) {
+                                                DwRed<NUM, WAVES>& red) {
   constexpr int PIECE = NUM::PIECE;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
   const int col = slice * NUM::COLS + PIECE * n;
   const int col_at = PIECE == 8 ? min(col, hidden - 8) : col;  // (fp32 rows of any length are checked where they are read)
   const int e0 = 16 * M * tile, e = e0 + M * n;
-  const bool whole_e = n_experts % 4 == 0, whole_h = hidden % 4 == 0;
   f32x4_t acc[M][PIECE];
 #pragma unroll
   for (int m = 0; m < M; ++m)
 #pragma unroll
     for (int i = 0; i < PIECE; ++i) acc[m][i] = f32x4_t{0, 0, 0, 0};
-  constexpr int STRIDE = DW_WAVES * NUM::STEP;
+  constexpr int STRIDE = WAVES * NUM::STEP, RING = AHEAD + 1;
   int t = t_begin + wave * NUM::STEP;
-  if constexpr (M == 1) {  // few blocks: the next step is on its way too
-    if (t < t_end) {
-      DwStep<NUM, M> ahead;
-      ahead.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
-      for (; t < t_end; t += STRIDE) {
-        DwStep<NUM, M> step = ahead;
-        if (t + STRIDE < t_end) ahead.load(x, d_logits, t + STRIDE, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
-        step.multiply(acc, t_end - t, kblk);
+  if (t < t_end) {
+    DwStep<NUM, M, WHOLE> ring[RING];
+    // (steps past the end load its last token; nothing multiplies them)
+    auto load = [&](DwStep<NUM, M, WHOLE>& step, int t0) {
+      step.load(x, d_logits, t0, t_end, col_at, e, n_experts, hidden, kblk);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(ring[i], t + i * STRIDE);
+    for (bool more = true; more;) {
+#pragma unroll
+      for (int i = 0; i < RING; ++i) {
+        if (more) {
+          load(ring[(i + AHEAD) % RING], t + AHEAD * STRIDE);
+          __builtin_amdgcn_sched_barrier(0);  // (left alone, the loads move down to their uses)
+          ring[i].multiply(acc, t_end - t, kblk);
+          t += STRIDE;
+          more = t < t_end;
+        }
       }
-    }
-  } else {
-    for (; t < t_end; t += STRIDE) {
-      DwStep<NUM, M> step;
-      step.load(x, d_logits, t, t_end, col_at, e, n_experts, hidden, whole_e, whole_h, kblk);
-      step.multiply(acc, t_end - t, kblk);
     }
   }
   // register r of lane (n, kblk) is row 4 kblk + r of the instruction: expert e0 + M (4 kblk + r) + m; operand i column PIECE n + i
@@ -424,55 +437,60 @@ __device__ __forceinline__ void router_dw_block(const typename NUM::T* __restric
 #pragma unroll
       for (int r = 0; r < 4; ++r) red[wave][i * 4 + r][lane] = acc[m][i][r];
     __syncthreads();
-    // a thread per row and half of its piece of columns
-    constexpr int HALF = PIECE / 2;
-    static_assert(DW_WAVES == 8, "");
-    const int r = wave % 4, i0 = wave / 4 * HALF, to = e0 + M * (4 * kblk + r) + m;
-    float v[HALF];
+    // a thread per row and some of its piece of columns
+    constexpr int SOME = PIECE * 4 / WAVES;
+    static_assert(WAVES % 4 == 0 && SOME >= 1, "");
+    const int r = wave % 4, i0 = wave / 4 * SOME, to = e0 + M * (4 * kblk + r) + m;
+    float v[SOME];
 #pragma unroll
-    for (int i = 0; i < HALF; ++i) {
+    for (int i = 0; i < SOME; ++i) {
       v[i] = red[0][(i0 + i) * 4 + r][lane];
 #pragma unroll
-      for (int w = 1; w < DW_WAVES; ++w) v[i] += red[w][(i0 + i) * 4 + r][lane];
+      for (int w = 1; w < WAVES; ++w) v[i] += red[w][(i0 + i) * 4 + r][lane];
     }
     if (to < n_experts) {
       float* row = out + (size_t)to * hidden;
-      if (PIECE == 8) {  // (columns come in eights)
-        if (col < hidden) *(f32x4_t*)(row + col + i0) = f32x4_t{v[0], v[1], v[2 % HALF], v[3 % HALF]};
+      if constexpr (PIECE == 8) {  // (columns come in eights)
+#pragma unroll
+        for (int i = 0; i < SOME; i += 4)
+          if (col < hidden) *(f32x4_t*)(row + col + i0 + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
       } else {
 #pragma unroll
-        for (int i = 0; i < HALF; ++i)
+        for (int i = 0; i < SOME; ++i)
           if (col + i0 + i < hidden) row[col + i0 + i] = v[i];
       }
     }
   }
 }
 
-template <class NUM>
-__global__ __launch_bounds__(64 * DW_WAVES, 2) void router_dw_kernel(const typename NUM::T* __restrict__ x, const float* __restrict__ d_logits,
+// One wave per SIMD with two steps ahead (16384 tokens, 64 experts of 2048, from memory: 37 us with two waves and none -> DW_US).
+constexpr int DW_WAVES = 4;
+template <class NUM, bool WHOLE>
+__global__ __launch_bounds__(64 * DW_WAVES, 1) void router_dw_kernel(const typename NUM::T* __restrict__ x, const float* __restrict__ d_logits,
                                                                      int n_tokens, int n_experts, int hidden, int chunk_tokens,
                                                                      float* __restrict__ out) {
-  __shared__ DwRed<NUM> red;
+  __shared__ DwRed<NUM, DW_WAVES> red;
   const int t_begin = blockIdx.y * chunk_tokens;
-  router_dw_block<NUM, 4>(x, d_logits, n_experts, hidden, blockIdx.x, blockIdx.z, t_begin, min(t_begin + chunk_tokens, n_tokens),
+  router_dw_block<NUM, 4, DW_WAVES, 2, WHOLE>(x, d_logits, n_experts, hidden, blockIdx.x, blockIdx.z, t_begin, min(t_begin + chunk_tokens, n_tokens),
                           out + (size_t)blockIdx.y * n_experts * hidden, red);
 }
 
 // Batches of up to SMALL_TOKENS: both results in one launch, d_w_g without chunks.  The first dw_blocks blocks are d_w_g's (they
 // take longest), the others eight waves of dx.
-template <class NUM>
-__global__ __launch_bounds__(64 * DW_WAVES, 2) void router_backward_small_kernel(const typename NUM::T* __restrict__ x,
+constexpr int SMALL_WAVES = 8;
+template <class NUM, bool WHOLE>
+__global__ __launch_bounds__(64 * SMALL_WAVES, 2) void router_backward_small_kernel(const typename NUM::T* __restrict__ x,
                                                                                  const typename NUM::T* __restrict__ w_g,
                                                                                  const float* __restrict__ d_logits, int n_tokens, int n_experts,
                                                                                  int hidden, const typename NUM::T* add, typename NUM::T* dx,
                                                                                  float* __restrict__ d_w_g, int slices, int dw_blocks) {
-  __shared__ DwRed<NUM> red;
+  __shared__ DwRed<NUM, SMALL_WAVES> red;
   const int b = blockIdx.x;
   if (b < dw_blocks) {
-    router_dw_block<NUM, 1>(x, d_logits, n_experts, hidden, b % slices, b / slices, 0, n_tokens, d_w_g, red);
+    router_dw_block<NUM, 1, SMALL_WAVES, 1, WHOLE>(x, d_logits, n_experts, hidden, b % slices, b / slices, 0, n_tokens, d_w_g, red);
   } else {
-    const int i = b - dw_blocks, t0 = (i / slices * DW_WAVES + threadIdx.x / 64) * 16;
-    if (t0 < n_tokens) router_dx_wave(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, i % slices);
+    const int i = b - dw_blocks, t0 = (i / slices * SMALL_WAVES + threadIdx.x / 64) * 16;
+    if (t0 < n_tokens) router_dx_wave<WHOLE>(w_g, d_logits, add, n_tokens, n_experts, hidden, dx, t0, i % slices);
   }
 }
 
@@ -513,25 +531,25 @@ static DwPlan dw_plan(const hmoe_layer_desc& d, int T) {
   return p;
 }
 
-template <class NUM>
+template <class NUM, bool WHOLE>
 static void launch_router_backward(const hmoe_layer_desc& d, const typename NUM::T* x, const typename NUM::T* w_g, const float* d_logits, int T,
                                    const typename NUM::T* add, typename NUM::T* dx, float* d_w_g, float* workspace, hipStream_t s) {
   const int E = d.n_experts, H = d.hidden;
   const DwPlan p = dw_plan(d, T);
   if (T <= SMALL_TOKENS) {
-    const int dw_blocks = d_w_g ? p.slices * ((E + 15) / 16) : 0, dx_blocks = dx ? p.slices * ((T + 16 * DW_WAVES - 1) / (16 * DW_WAVES)) : 0;
+    const int dw_blocks = d_w_g ? p.slices * ((E + 15) / 16) : 0, dx_blocks = dx ? p.slices * ((T + 16 * SMALL_WAVES - 1) / (16 * SMALL_WAVES)) : 0;
     if (dw_blocks + dx_blocks > 0)
-      hipLaunchKernelGGL(router_backward_small_kernel<NUM>, dim3((unsigned)(dw_blocks + dx_blocks)), dim3(64 * DW_WAVES), 0, s, x, w_g, d_logits,
+      hipLaunchKernelGGL((router_backward_small_kernel<NUM, WHOLE>), dim3((unsigned)(dw_blocks + dx_blocks)), dim3(64 * SMALL_WAVES), 0, s, x, w_g, d_logits,
                          T, E, H, add, dx, d_w_g, p.slices, dw_blocks);
     return;
   }
   if (dx) {
-    hipLaunchKernelGGL(router_dx_kernel<NUM>, dim3((unsigned)((T + 63) / 64), (unsigned)p.slices), dim3(256), 0, s, w_g, d_logits, add, T, E, H,
+    hipLaunchKernelGGL((router_dx_kernel<NUM, WHOLE>), dim3((unsigned)((T + 63) / 64), (unsigned)p.slices), dim3(256), 0, s, w_g, d_logits, add, T, E, H,
                        dx);
   }
   if (d_w_g) {
     const dim3 grid((unsigned)p.slices, (unsigned)p.chunks, (unsigned)p.tiles);
-    hipLaunchKernelGGL(router_dw_kernel<NUM>, grid, dim3(64 * DW_WAVES), 0, s, x, d_logits, T, E, H, p.chunk_tokens,
+    hipLaunchKernelGGL((router_dw_kernel<NUM, WHOLE>), grid, dim3(64 * DW_WAVES), 0, s, x, d_logits, T, E, H, p.chunk_tokens,
                        p.chunks > 1 ? workspace : d_w_g);
     if (p.chunks > 1) {
       const long n = (long)E * H;
@@ -613,11 +631,13 @@ extern "C" int32_t hmoe_router_backward(const hmoe_layer_desc* desc, const void*
   if (!workspace || workspace_bytes < hmoe_router_backward_workspace_bytes(desc, T)) return HMOE_ERR_WORKSPACE;
   if (!aligned16(workspace)) return HMOE_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
-  if (desc->dtype == HMOE_F32)
-    launch_router_backward<DwF32>(*desc, (const float*)x, (const float*)w_g, d_logits, T, (const float*)add, (float*)dx, d_w_g, (float*)workspace, s);
-  else
-    launch_router_backward<DwBf16>(*desc, (const bf16_t*)x, (const bf16_t*)w_g, d_logits, T, (const bf16_t*)add, (bf16_t*)dx, d_w_g,
-                                   (float*)workspace, s);
+  auto launch = [&](auto num, auto launch_of) {
+    typedef typename decltype(num)::T V;
+    launch_of(*desc, (const V*)x, (const V*)w_g, d_logits, T, (const V*)add, (V*)dx, d_w_g, (float*)workspace, s);
+  };
+  const bool rows_of_4 = desc->n_experts % 4 == 0 && desc->hidden % 4 == 0;
+  if (desc->dtype == HMOE_F32) launch(DwF32{}, rows_of_4 ? &launch_router_backward<DwF32, true> : &launch_router_backward<DwF32, false>);
+  else launch(DwBf16{}, rows_of_4 ? &launch_router_backward<DwBf16, true> : &launch_router_backward<DwBf16, false>);
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;
 }
