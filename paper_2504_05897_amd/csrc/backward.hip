@@ -182,46 +182,43 @@ struct DwF32 {
   static constexpr int COLS = 64, PIECE = 4, STEP = 16;
 };
 
-// dx, bfloat16: a wave takes 16 tokens from t0 x 128 columns (slice) and goes through the experts 32 at a time.  (32 tokens for
-// each load of W_g: 69 against 68 us for gates and router of 16384 tokens; the more waves that fit hide more.)
-template <bool WHOLE>
-__device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits, const bf16_t* add,
-                                               int n_tokens, int n_experts, int hidden, bf16_t* dx, int t0, int slice) {
-  const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
-  const int col = slice * DwBf16::COLS + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
-  f32x4_t acc[8];
+// dx, bfloat16: a wave has 16 tokens x 128 columns (slice) and goes through the experts 32 at a time.
+//
+// W_g rows e .. + 8 of the lane's k block, eight columns from col_at, as operands; rows past the last are zeros: they meet a
+// value of the token's own row, and if that is infinite, so is the token's result already.
+__device__ __forceinline__ void load_w_rows(u32x4 (&w)[8], const bf16_t* __restrict__ w_g, int e, int n_experts, int hidden, int col_at) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
-  u32x4 more[4];  // `add`, on its way while the experts are multiplied
-  if (add) {
+  for (int k = 0; k < 8; ++k) w[k] = *(const u32x4*)(w_g + (size_t)min(e + k, n_experts - 1) * hidden + col_at);
+}
+__device__ __forceinline__ void w_operands(u32x4 (&w)[8], u32x4 (&op)[8], int e0, int kblk, int n_experts) {
+  if (e0 + 32 > n_experts) {  // uniform
 #pragma unroll
-    for (int r = 0; r < 4; ++r) more[r] = __builtin_nontemporal_load((const u32x4*)(add + (size_t)min(t0 + 4 * kblk + r, n_tokens - 1) * hidden + col_at));
+    for (int k = 0; k < 8; ++k)
+      if (e0 + 8 * kblk + k >= n_experts) w[k] = u32x4{0, 0, 0, 0};
   }
-  const float* row = d_logits + (size_t)min(t0 + n, n_tokens - 1) * n_experts;
-  for (int e0 = 0; e0 < n_experts; e0 += 32) {
-    const int e = e0 + 8 * kblk;
-    u32x4 w[8], op[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = *(const u32x4*)(w_g + (size_t)min(e + k, n_experts - 1) * hidden + col_at);
-    const f32x4_t d0 = load_4<WHOLE>(row, e, n_experts), d1 = load_4<WHOLE>(row, e + 4, n_experts);
-    if (e0 + 32 > n_experts) {  // uniform
-#pragma unroll
-      for (int k = 0; k < 8; ++k)  // (meets a value of the token's own row: if that is infinite, so is the token's result already)
-        if (e + k >= n_experts) w[k] = u32x4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const uint32_t rows[8] = {w[0][p], w[1][p], w[2][p], w[3][p], w[4][p], w[5][p], w[6][p], w[7][p]};
-      transpose_halves(rows, op[2 * p], op[2 * p + 1]);
-    }
-    float v[8] = {d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
-    const u32x4 hi = take_piece(v), lo = round_piece(v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(hi, op[i], acc[i]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(lo, op[i], acc[i]);
+  for (int p = 0; p < 4; ++p) {
+    const uint32_t rows[8] = {w[0][p], w[1][p], w[2][p], w[3][p], w[4][p], w[5][p], w[6][p], w[7][p]};
+    transpose_halves(rows, op[2 * p], op[2 * p + 1]);
   }
-  // register r of lane (n, kblk) is token 4 kblk + r, operand i column 8 n + i
+}
+__device__ __forceinline__ void add_experts(f32x4_t (&acc)[8], const f32x4_t& d0, const f32x4_t& d1, const u32x4 (&op)[8]) {
+  float v[8] = {d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+  const u32x4 hi = take_piece(v), lo = round_piece(v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(hi, op[i], acc[i]);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(lo, op[i], acc[i]);
+}
+// what is added to rows t0 + 4 kblk .. + 4
+__device__ __forceinline__ void load_more(u32x4 (&more)[4], const bf16_t* add, int t0, int kblk, int n_tokens, int hidden, int col_at) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    more[r] = __builtin_nontemporal_load((const u32x4*)(add + (size_t)min(t0 + 4 * kblk + r, n_tokens - 1) * hidden + col_at));
+}
+// register r of lane (n, kblk) is token 4 kblk + r, operand i column 8 n + i
+__device__ __forceinline__ void store_dx(const f32x4_t (&acc)[8], const u32x4 (&more)[4], bool added, bf16_t* dx, int t0, int kblk, int n_tokens,
+                                         int hidden, int col) {
   if (col >= hidden) return;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -230,7 +227,7 @@ __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, c
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = acc[i][r];
-    if (add) {
+    if (added) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[2 * i] += __uint_as_float(more[r][i] << 16);
@@ -238,6 +235,73 @@ __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, c
       }
     }
     __builtin_nontemporal_store(round_piece(v), (u32x4*)(dx + (size_t)t * hidden + col));
+  }
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits, const bf16_t* add,
+                                               int n_tokens, int n_experts, int hidden, bf16_t* dx, int t0, int slice) {
+  const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int col = slice * DwBf16::COLS + 8 * n, col_at = min(col, hidden - 8);  // clamped: never stored
+  f32x4_t acc[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
+  u32x4 more[4];  // on its way while the experts are multiplied
+  if (add) load_more(more, add, t0, kblk, n_tokens, hidden, col_at);
+  const float* row = d_logits + (size_t)min(t0 + n, n_tokens - 1) * n_experts;
+  for (int e0 = 0; e0 < n_experts; e0 += 32) {
+    const int e = e0 + 8 * kblk;
+    u32x4 w[8], op[8];
+    load_w_rows(w, w_g, e, n_experts, hidden, col_at);
+    const f32x4_t d0 = load_4<WHOLE>(row, e, n_experts), d1 = load_4<WHOLE>(row, e + 4, n_experts);
+    w_operands(w, op, e0, kblk, n_experts);
+    add_experts(acc, d0, d1, op);
+  }
+  store_dx(acc, more, add != nullptr, dx, t0, kblk, n_tokens, hidden, col);
+}
+
+// Large batches over at most 32 EC experts: a wave keeps its columns of W_g as operands and goes from one 16 tokens to another,
+// the next ones on their way.  16384 tokens, 64 experts of 2048, from memory: 31 us, 4.5 TB/s; with W_g read
+// for every 16 tokens 39.
+template <int EC, bool WHOLE>
+__global__ __launch_bounds__(256, EC <= 2 ? 2 : 1) void router_dx_walk_kernel(const bf16_t* __restrict__ w_g, const float* __restrict__ d_logits,
+                                                                              const bf16_t* add, int n_tokens, int n_experts, int hidden,
+                                                                              bf16_t* dx) {
+  const int lane = threadIdx.x % 64, n = lane % 16, kblk = lane / 16;
+  const int col = blockIdx.y * DwBf16::COLS + 8 * n, col_at = min(col, hidden - 8);
+  struct Tokens {
+    f32x4_t d[EC][2];
+    u32x4 more[4];
+  } now, next;
+  auto load = [&](Tokens& k, int t0) {
+    const float* row = d_logits + (size_t)min(t0 + n, n_tokens - 1) * n_experts;
+#pragma unroll
+    for (int c = 0; c < EC; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) k.d[c][i] = load_4<WHOLE>(row, 32 * c + 8 * kblk + 4 * i, n_experts);
+    if (add) load_more(k.more, add, t0, kblk, n_tokens, hidden, col_at);
+  };
+  const int stride = gridDim.x * 64;
+  int t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 16;
+  if (t0 >= n_tokens) return;
+  u32x4 op[EC][8];
+  load(next, t0);
+#pragma unroll
+  for (int c = 0; c < EC; ++c) {
+    u32x4 w[8];
+    load_w_rows(w, w_g, 32 * c + 8 * kblk, n_experts, hidden, col_at);
+    w_operands(w, op[c], 32 * c, kblk, n_experts);
+  }
+  for (; t0 < n_tokens; t0 += stride) {
+    now = next;
+    load(next, min(t0 + stride, n_tokens - 1));  // (past the end: its last token again, unused)
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4_t acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < EC; ++c) add_experts(acc, now.d[c][0], now.d[c][1], op[c]);
+    store_dx(acc, now.more, add != nullptr, dx, t0, kblk, n_tokens, hidden, col);
   }
 }
 
@@ -463,7 +527,7 @@ __device__ __forceinline__ void router_dw_block(const typename NUM::T* __restric
   }
 }
 
-// One wave per SIMD with two steps ahead (16384 tokens, 64 experts of 2048, from memory: 37 us with two waves and none -> DW_US).
+// One wave per SIMD with two steps ahead (16384 tokens, 64 experts of 2048, from memory: 22 us; two waves without: 37).
 constexpr int DW_WAVES = 4;
 template <class NUM, bool WHOLE>
 __global__ __launch_bounds__(64 * DW_WAVES, 1) void router_dw_kernel(const typename NUM::T* __restrict__ x, const float* __restrict__ d_logits,
@@ -544,8 +608,19 @@ static void launch_router_backward(const hmoe_layer_desc& d, const typename NUM:
     return;
   }
   if (dx) {
-    hipLaunchKernelGGL((router_dx_kernel<NUM, WHOLE>), dim3((unsigned)((T + 63) / 64), (unsigned)p.slices), dim3(256), 0, s, w_g, d_logits, add, T, E, H,
-                       dx);
+    const unsigned blocks = (unsigned)((T + 63) / 64);
+    auto launch = [&](auto kernel, unsigned most) {
+      hipLaunchKernelGGL(kernel, dim3(std::min(blocks, most), (unsigned)p.slices), dim3(256), 0, s, w_g, d_logits, add, T, E, H, dx);
+    };
+    const unsigned per_slice = (unsigned)std::max(1, 512 / p.slices);  // two blocks per CU
+    if constexpr (NUM::PIECE == 8) {
+      if (E <= 32) launch(&router_dx_walk_kernel<1, WHOLE>, per_slice);
+      else if (E <= 64) launch(&router_dx_walk_kernel<2, WHOLE>, per_slice);
+      else if (E <= 128) launch(&router_dx_walk_kernel<4, WHOLE>, (per_slice + 1) / 2);
+      else launch(&router_dx_kernel<NUM, WHOLE>, blocks);
+    } else {
+      launch(&router_dx_kernel<NUM, WHOLE>, blocks);
+    }
   }
   if (d_w_g) {
     const dim3 grid((unsigned)p.slices, (unsigned)p.chunks, (unsigned)p.tiles);

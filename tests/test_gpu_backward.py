@@ -331,3 +331,28 @@ def test_layer_without_a_router(hm):
     assert d_w is None and d_logits.shape == (6, 8) and torch.isfinite(d_logits).all()
     assert (d_logits.sum(1).abs() <= 1e-5 * d_logits.abs().sum(1) + 1e-12).all()      # softmax does not see a shift of all logits
     layer.close()
+
+
+@pytest.mark.parametrize("dtype,T,H,E", [("bf16", 2049, 272, 32), ("bf16", 9000, 144, 61), ("bf16", 2500, 1040, 64), ("bf16", 3001, 128, 97),
+                                         ("bf16", 2100, 80, 130), ("f32", 2049, 68, 20), ("f32", 5000, 37, 33)])
+def test_router_backward_of_large_batches(hm, dtype, T, H, E):
+    """Beyond the batches that one launch does: blocks that go from tokens to tokens, chunks of tokens, ends that are no multiples."""
+    say("router backward, large", dtype, T, H, E)
+    p = Problem(hm, dtype, T, H, E, 1, seed=8)
+    x, w_g, d, add = (to_device(a) for a in (p.x, p.w_g, p.d_logits, p.add))
+    n = hm.hmoe_router_backward_workspace_bytes(p.desc, T)
+    ws = torch.full((n + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    dx, d_w = p.empty(T + 1, H), p.empty(E + 1, H, dtype=torch.float32)
+    hm.hmoe_router_backward(p.desc, x, w_g, d, T, add, dx, d_w, ws, n)
+    torch.cuda.synchronize()
+    assert dx[T].isnan().all() and d_w[E].isnan().all() and (ws[n:] == 0x5a).all()
+    xv, wv, dv = p.value(p.x), p.value(p.w_g), p.d_logits.astype(np.float64)
+    ref_dx, ref_dw = go.router_backward(xv, wv, dv, p.value(p.add))
+    slack = ((E + 2) * U + (2.0 ** -17 if p.bf16 else 0)) * (np.abs(dv) @ np.abs(wv)) + 2 * U * np.abs(p.value(p.add))
+    assert (np.abs(to_host_f32(dx[:T]) - ref_dx) <= p.step * (np.abs(ref_dx) + slack) + slack).all()
+    assert (np.abs(to_host_f32(d_w[:E]) - ref_dw) <= (T + 2) * U * (np.abs(dv).T @ np.abs(xv))).all()
+    alone = p.empty(T, H)
+    hm.hmoe_router_backward(p.desc, None, w_g, d, T, None, alone, None, ws, n)
+    torch.cuda.synchronize()
+    ref = go.router_backward(xv, wv, dv)[0]
+    assert (np.abs(to_host_f32(alone) - ref) <= p.step * (np.abs(ref) + slack) + slack).all()
