@@ -374,3 +374,60 @@ def test_codes_once_per_token(hm, T, far):
         torch.cuda.synchronize()
         assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and a.isfinite().all() and (ws[n:] == 0x5a).all()
     layer.close()
+
+
+def test_large_batch_through_a_partial_cache_and_a_graph(hm):
+    """A batch whose tokens are quantised once each: with half of the experts staged wave by wave, and captured and replayed, the
+    bits of an eager call with every expert resident."""
+    say("i8 large batch, partial cache, graph")
+    T, H, F, E, K = 4300, 1024, 256, 8, 2
+    shape = wl.small_shape(dtype=wl.BF16, hidden=H, ffn=F, n_experts=E, top_k=K, x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 21, T)
+    assert T * K * H >= 8 << 20
+    whole = hm.MoELayer(hm.make_desc(H, F, E, K, E, hm.HMOE_BF16_I8), lay.experts, (), lay.w_router, max_tokens=T)
+    half = hm.MoELayer(hm.make_desc(H, F, E, K, 3, hm.HMOE_BF16_I8), lay.experts, (), lay.w_router, max_tokens=T)
+    x = to_device(lay.x)
+    want = whole.forward(x).clone()
+    got = half.forward(x)
+    torch.cuda.synchronize()
+    assert torch.equal(got.view(torch.int16), want.view(torch.int16)) and half.last_plan[3] > 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = whole.forward(x)
+    for seed in range(2):
+        x.copy_(to_device(rows_of(40 + seed, T, H)))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = y.clone()
+        assert torch.equal(replayed.view(torch.int16), whole.forward(x).view(torch.int16)), seed
+    idx, w = whole.topk_idx[:4].cpu().numpy(), whole.topk_w[:4].cpu().numpy()
+    f64 = [tuple(wl.as_f64(m) for m in e) for e in lay.experts]
+    ref, bound = i8.moe_layer(wl.as_f64(rows_of(41, T, H)[:4]), idx, w, f64)
+    assert (np.abs(to_host_f32(y[:4]) - ref) <= bound).all()
+    whole.close()
+    half.close()
+
+
+def test_two_calls_at_once(hm):
+    """Two layers' calls on two streams, each with a workspace of its own, again and again: nothing is shared."""
+    say("i8 two calls at once")
+    counts = [200, 90, 0, 300]
+    made = [make(hm, 512, 384, 4, 1, seed, distinct=2) for seed in (31, 32)]
+    xs = [to_device(rows_of(50 + i, sum(counts), 512)) for i in range(2)]
+    offsets = to_device(offsets_of(counts))
+    A = sum(counts)
+    want = [grouped(hm, d, layer, x, offsets, A, TILED) for (d, _, layer), x in zip(made, xs)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    n = hm.hmoe_ffn_workspace_bytes(made[0][0], A)
+    ws = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    outs = [[torch.empty_like(want[0]) for _ in range(6)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for k in range(6):
+        for i, (d, _, layer) in enumerate(made):
+            hm.hmoe_expert_ffn_grouped(d, layer.cache, xs[i], offsets, A, None, outs[i][k], ws[i], n, TILED, streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in outs[i]:
+            assert torch.equal(o.view(torch.int16), want[i].view(torch.int16))
+    for _, _, layer in made:
+        layer.close()
