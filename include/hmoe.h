@@ -81,8 +81,8 @@ enum { HMOE_F32 = 0, HMOE_BF16 = 1, HMOE_BF16_W4 = 2, HMOE_BF16_I8 = 3 };
  * are rounded to bfloat16 once.  A row of zeros has codes 0; a row that holds an infinity or a NaN makes every result that
  * it takes part in NaN.  The sums being exact, results do not depend on the number of tokens or the path beyond the last
  * bits of silu (HMOE_FFN_REFERENCE divides and takes expf).
- * Needs H % 128 == 0 and F % 128 == 0.  FFN paths: HMOE_FFN_SKINNY (AUTO up to 16 tokens, in small layers while an
- * expert has few rows), HMOE_FFN_TILED (AUTO above) and HMOE_FFN_REFERENCE.  Everything else (router, route, permute, combine) behaves as for HMOE_BF16.
+ * Needs H % 128 == 0 and F % 128 == 0.  FFN paths: HMOE_FFN_SKINNY (AUTO up to 16 tokens, in small layers up to
+ * 256), HMOE_FFN_TILED (AUTO above) and HMOE_FFN_REFERENCE.  Everything else (router, route, permute, combine) behaves as for HMOE_BF16.
  */
 
 /* Which FFN kernels hmoe_expert_ffn_grouped uses.  AUTO picks by token count. */
@@ -307,7 +307,7 @@ int32_t hmoe_route_scores(const hmoe_layer_desc* desc, const float* logits, int3
  *       resident are left untouched.
  *   workspace: hmoe_ffn_workspace_bytes(desc, A) bytes of device scratch (holds h [A, F]; for HMOE_BF16_I8 h in fp32, the
  *       codes of the rows at hand and their scales).
- *   path: HMOE_FFN_*; AUTO = SKINNY when T = A/K <= 32 (4-bit weights and 8-bit integers: 16) else TILED; for fp32 tiles of their own
+ *   path: HMOE_FFN_*; AUTO = SKINNY when T = A/K <= 32 (4-bit weights: 16, 8-bit integers: see HMOE_BF16_I8) else TILED; for fp32 tiles of their own
  *       when H and F are multiples of 4 and there are more than a few rows, else REFERENCE (the only path by name).
  * Shared experts (Section II-A) use the same call with a 1-expert layer (E = K = S = 1,
  * offsets {0, T}).

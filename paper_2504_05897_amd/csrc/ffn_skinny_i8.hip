@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * NW) void ffn_skinny_i8_kernel(SkinnyI8Ctx c, c
   constexpr uint32_t NO_ROW = 0xF0000000u;
 
   const int PASS = OWN ? c.own_rows : 16 * XF;
-  for (int row0 = row_first; row0 < row_end; row0 += PASS) {
+  for (int row0 = row_first + (int)blockIdx.z * PASS; row0 < row_end; row0 += PASS * (int)gridDim.z) {
     const int rows = min(PASS, row_end - row0);
     uint32_t xin[XF];
 #pragma unroll
@@ -200,8 +200,11 @@ __global__ __launch_bounds__(64 * NW) void ffn_skinny_i8_kernel(SkinnyI8Ctx c, c
 // 37.8 / 37.0 / 38.9, over 64 steps, 2 experts, 40.5 / 39.7 / 41.2; down over 22 steps 21.7 / 22.5 / 27.4, over 224 steps, 2
 // experts, 38.6 / 25.7 / 22.4).
 template <bool GATEUP, int XF, bool OWN>
-static void launch_stage_i8(const SkinnyI8Ctx& c, int busy_max, const void* in, const float* row_scales, void* out, hipStream_t s) {
-  const dim3 grid((unsigned)((GATEUP ? c.ffn : c.hidden) / TILE_N), (unsigned)busy_max);
+static void launch_stage_i8(const SkinnyI8Ctx& c, int busy_max, int max_rows, const void* in, const float* row_scales, void* out,
+                            hipStream_t s) {
+  // (an expert's passes side by side, so that one with many rows does not take as many times as long)
+  const unsigned passes = OWN ? 1 : (unsigned)std::min(8, (max_rows + 16 * XF - 1) / (16 * XF));
+  const dim3 grid((unsigned)((GATEUP ? c.ffn : c.hidden) / TILE_N), (unsigned)busy_max, passes);
   const int K = GATEUP ? c.hidden : c.ffn, n_steps = K / 64;
   const size_t lds = OWN ? (size_t)c.own_rows * (K + SKINNY_I8_ROW_PAD) : 0;
   auto launch = [&](auto kernel, int nw) { hipLaunchKernelGGL(kernel, grid, dim3(64 * nw), lds, s, c, in, row_scales, out); };
@@ -212,13 +215,17 @@ static void launch_stage_i8(const SkinnyI8Ctx& c, int busy_max, const void* in, 
 
 // What HMOE_FFN_AUTO chooses (calls, us, these kernels / the prefill tiles): up to 16 tokens (64 experts of 3584 x 2560, top 8, 16 tokens
 // 246 / 256, 32 tokens 288 / 277; 8 of 4096 x 14336, top 2, 20 tokens 226 / 226; 64 of 2048 x 1408, top 6, 20 tokens 93 / 88; one of 3584 x
-// 20480, 16 tokens 65 / 75, 32 tokens 82 / 77), and for small layers, whose calls are a few launches' latency, while an expert's
-// rows fit a pass (16 of 1024 x 640, top 2, 77 tokens 19.0 / 21.1, 120 tokens 20.3 / 21.2, 200 tokens 24.2 / 21.9; one of 2048 x 2816, 32
-// tokens 24.6 / 29.3, 48 tokens 34.6 / 29.7).
+// 20480, 16 tokens 65 / 75, 32 tokens 82 / 77).  Small layers, whose calls are a few launches' latency, up to 256 tokens while that is no
+// more than a few rounds of blocks (16 of 1024 x 640, top 2, 77 / 200 tokens 19.6 / 22.2, 23.8 / 22.9, with skewed routing 21.3 / 22.0, 27.3 /
+// 34.3; one of 2048 x 2816, 48 / 256 tokens 24 / 30, 38 / 49; one of 2048 x 8192, 64 / 128 tokens 39 / 43, 48 / 54; but 71 of 2304 x 128, top 3, 229
+// tokens, 40896 blocks, 48 / 44; 85 of 128 x 1792, top 7, 24 tokens, 4760 blocks, 26 / 23, 187 tokens, 28560 blocks, 75 / 37), whose
+// passes of 32 rows do not read the weights too often (one of 4096 x 5120, 64 / 200 tokens 43 / 48, 98 / 82).
 bool ffn_skinny_i8_takes(const hmoe_layer_desc& d, int n_rows) {
   const int T = n_rows / d.top_k;
   if (T <= 16) return true;
-  return 3l * d.hidden * d.ffn * d.n_experts <= (64l << 20) && (T <= 32 || n_rows <= 16 * d.n_experts);
+  const long passes = (T + 31) / 32, bytes = 3l * d.hidden * d.ffn * d.n_experts;
+  if (T > 256 || bytes > (64l << 20) || bytes * passes > (256l << 20)) return false;
+  return (long)(std::max(d.hidden, d.ffn) / TILE_N) * std::min(d.n_experts, n_rows) * passes <= 4096;
 }
 
 int launch_ffn_skinny_i8(const FfnArgs& a) {
@@ -248,14 +255,14 @@ int launch_ffn_skinny_i8(const FfnArgs& a) {
   c.own_rows = max_rows;
   if (!own_x) launch_quantize_x_i8(a);
   probe_before(a.stream);
-  if (own_x) launch_stage_i8<true, 1, true>(c, busy_max, a.x_perm, nullptr, a.h, a.stream);
-  else (two ? launch_stage_i8<true, 2, false> : launch_stage_i8<true, 1, false>)(c, busy_max, codes, scales, a.h, a.stream);
+  if (own_x) launch_stage_i8<true, 1, true>(c, busy_max, max_rows, a.x_perm, nullptr, a.h, a.stream);
+  else (two ? launch_stage_i8<true, 2, false> : launch_stage_i8<true, 1, false>)(c, busy_max, max_rows, codes, scales, a.h, a.stream);
   probe_after(a.stream);
   if (!own_h) launch_quantize_h_i8(a);
   c.in_bytes = (uint32_t)h_bytes;
   probe_before(a.stream);
-  if (own_h) launch_stage_i8<false, 1, true>(c, busy_max, a.h, nullptr, a.o_perm, a.stream);
-  else (two ? launch_stage_i8<false, 2, false> : launch_stage_i8<false, 1, false>)(c, busy_max, codes, scales, a.o_perm, a.stream);
+  if (own_h) launch_stage_i8<false, 1, true>(c, busy_max, max_rows, a.h, nullptr, a.o_perm, a.stream);
+  else (two ? launch_stage_i8<false, 2, false> : launch_stage_i8<false, 1, false>)(c, busy_max, max_rows, codes, scales, a.o_perm, a.stream);
   probe_after(a.stream);
   HMOE_HIP(hipGetLastError());
   return HMOE_OK;
