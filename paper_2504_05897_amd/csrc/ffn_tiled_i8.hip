@@ -12,15 +12,18 @@
 
 namespace hmoe {
 
-template <class TILE, class OUT>
-__device__ __forceinline__ void run_tile_i8(const TiledCtx& c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
-                                            OUT* __restrict__ out, const TileLoc& loc, u32x4* lds) {
-  typename TILE::Acc acc;
+template <class TILE>
+__device__ __forceinline__ void clear_sums(typename TILE::Acc& acc) {
 #pragma unroll
   for (int i = 0; i < TILE::FM; ++i)
 #pragma unroll
     for (int j = 0; j < TILE::FN; ++j) acc[i][j] = i32x16_t{0};
-  TILE::mainloop(c, in, loc, 0, TILE::k_units(c) / TILE::BKT, lds, acc);
+}
+
+// The tile's integer sums times their scales, to `out` as h or o_perm.
+template <class TILE, class OUT>
+__device__ __forceinline__ void finish_tile_i8(const TiledCtx& c, const float* __restrict__ row_scales, OUT* __restrict__ out, const TileLoc& loc,
+                                               const typename TILE::Acc& acc, u32x4* lds) {
   // scales of the lane's column in each of the wave's groups (of group 0 for groups past N: never stored)
   const int wave = threadIdx.x / 64, col = threadIdx.x % 32;
   const char* slot = c.slots + (size_t)loc.slot * c.slot_bytes;
@@ -40,6 +43,15 @@ __device__ __forceinline__ void run_tile_i8(const TiledCtx& c, const bf16_t* __r
   else if constexpr (TILE::GATEUP) TILE::epilogue_pairs(c, out, loc, sums, lds);
   else if constexpr (TILE::FN == 2) TILE::epilogue_lines_down(c, out, loc, sums, lds);
   else TILE::epilogue_lines_block(c, out, loc, sums, lds);
+}
+
+template <class TILE, class OUT>
+__device__ __forceinline__ void run_tile_i8(const TiledCtx& c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
+                                            OUT* __restrict__ out, const TileLoc& loc, u32x4* lds) {
+  typename TILE::Acc acc;
+  clear_sums<TILE>(acc);
+  TILE::mainloop(c, in, loc, 0, TILE::k_units(c) / TILE::BKT, lds, acc);
+  finish_tile_i8<TILE>(c, row_scales, out, loc, acc, lds);
 }
 
 template <bool GATEUP, int BM, int NWV, bool NT, int RING, int FM, int FN>
@@ -76,6 +88,56 @@ __global__ __launch_bounds__(64 * NWV) void ffn_tile256_i8_kernel(TiledCtx c, co
   else if (fragments > 4) run_tile_i8<TileI8<GATEUP, 256, NWV, NT, 8, 6, 1>>(c, in, row_scales, out, loc, lds);
   else if (fragments > 2) run_tile_i8<TileI8<GATEUP, 256, NWV, NT, 8, 4, 1>>(c, in, row_scales, out, loc, lds);
   else run_tile_i8<TileI8<GATEUP, 256, NWV, NT, 8, 2, 1>>(c, in, row_scales, out, loc, lds);
+}
+
+// Down launches with a long K and a tile or less per CU: tiles of up to 160 rows x 128 columns, by two sets of four waves that take
+// half of K each (with one set, a SIMD has one wave, and nothing hides what that waits for).  The second set hands its sums to the
+// first, exact as they are, and ends.
+template <bool NT, int FM>
+using SplitI8 = StreamTile<false, 160, 4, 3, NT, 8, FM, 1, false, false, StreamI8>;
+constexpr int SPLIT_LDS = 2 * SplitI8<false, 5>::LDS_VEC;
+
+template <class TILE>
+__device__ __forceinline__ void run_split_i8(const TiledCtx& c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
+                                             bf16_t* __restrict__ out, const TileLoc& loc, u32x4* lds) {
+  static_assert(TILE::FM * 16 * 256 <= SPLIT_LDS * 4 && TILE::FN == 1, "the sums must fit");
+  const int set = __builtin_amdgcn_readfirstlane(threadIdx.x / 256), tid = threadIdx.x % 256;
+  const int half = TILE::k_units(c) / TILE::BKT / 2;
+  typename TILE::Acc acc;
+  clear_sums<TILE>(acc);
+  TILE::mainloop_of_set(c, in, loc, set * half, half, lds + set * TILE::LDS_VEC, acc, tid);
+  i32x4_t* sums = (i32x4_t*)lds + tid;
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  block_barrier();  // every wave has read its last activation fragments
+  if (set == 1) {
+#pragma unroll
+    for (int i = 0; i < TILE::FM * 4; ++i)
+      sums[i * 256] = i32x4_t{acc[i / 4][0][i % 4 * 4], acc[i / 4][0][i % 4 * 4 + 1], acc[i / 4][0][i % 4 * 4 + 2], acc[i / 4][0][i % 4 * 4 + 3]};
+  }
+  __syncthreads();
+  if (set == 1) return;
+#pragma unroll
+  for (int i = 0; i < TILE::FM * 4; ++i) {
+    const i32x4_t v = sums[i * 256];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[i / 4][0][i % 4 * 4 + t] += v[t];
+  }
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // before the barrier after which others write over the sums
+  finish_tile_i8<TILE>(c, row_scales, out, loc, acc, lds);
+}
+
+template <bool NT>
+__global__ __launch_bounds__(512) void ffn_tile_split_i8_kernel(TiledCtx c, const bf16_t* __restrict__ in, const float* __restrict__ row_scales,
+                                                                bf16_t* __restrict__ out) {
+  __shared__ u32x4 lds[SPLIT_LDS];
+  TileLoc loc;
+  if (!locate_tile<160>(c, loc)) return;  // uniform over the block
+  const int tiles = (loc.m_rows + 159) / 160;
+  const int fragments = ((loc.m_rows + tiles - 1) / tiles + 31) / 32;  // per m-tile, 1..5; uniform
+  if (fragments == 5) run_split_i8<SplitI8<NT, 5>>(c, in, row_scales, out, loc, lds);
+  else if (fragments == 4) run_split_i8<SplitI8<NT, 4>>(c, in, row_scales, out, loc, lds);
+  else if (fragments == 3) run_split_i8<SplitI8<NT, 3>>(c, in, row_scales, out, loc, lds);
+  else run_split_i8<SplitI8<NT, 2>>(c, in, row_scales, out, loc, lds);
 }
 
 // The 224x256 tile in blocks that work through several tiles, one wave per SIMD (see ffn_tile_walk_kernel).  A tile's last
@@ -242,7 +304,7 @@ __global__ __launch_bounds__(256) void ffn_tile_walk_i8_kernel(TiledCtx c, const
 }
 
 // Tile shapes.  nt: weight loads that are not kept in the caches.
-enum { I8_FIT4 = 0, I8_FIT256 = 1, I8_WALK = 2 };
+enum { I8_FIT4 = 0, I8_FIT256 = 1, I8_WALK = 2, I8_SPLIT = 6 };  // (the last: down only, a multiple of four K steps)
 
 template <bool GATEUP, class OUT>
 static void launch_stage_i8(TiledCtx c, int shape, bool nt, int n_rows, const bf16_t* in, const float* row_scales, OUT* out, hipStream_t s) {
@@ -260,6 +322,8 @@ static void launch_stage_i8(TiledCtx c, int shape, bool nt, int n_rows, const bf
     const auto kernel = odd ? (nt ? &ffn_tile_walk_i8_kernel<GATEUP, true, true, OUT> : &ffn_tile_walk_i8_kernel<GATEUP, false, true, OUT>)
                             : (nt ? &ffn_tile_walk_i8_kernel<GATEUP, true, false, OUT> : &ffn_tile_walk_i8_kernel<GATEUP, false, false, OUT>);
     launch(kernel, 224, 256, 256, 256);  // one block per CU
+  } else if (shape == I8_SPLIT) {
+    if constexpr (!GATEUP) launch(nt ? &ffn_tile_split_i8_kernel<true> : &ffn_tile_split_i8_kernel<false>, 160, 128, 512, ALL);
   } else if (shape == I8_FIT256) {
     launch(nt ? &ffn_tile256_i8_kernel<GATEUP, NW256, true, OUT> : &ffn_tile256_i8_kernel<GATEUP, NW256, false, OUT>, 256, 32 * NW256,
            64 * NW256, ALL);
@@ -274,6 +338,8 @@ static void launch_stage_i8(TiledCtx c, int shape, bool nt, int n_rows, const bf
 //     104 (66 and 140 rows of the first), 207 / 226 (128 of the second), 232 / 245 (62 of the third), 37 / 51 (1000 of the fourth); one
 //     expert of 3584 x 20480, 200 rows 41 / 50; but 20 rows of the second 167 / 157.  A down launch (66 rows of the first 49 / 44) has
 //     half the columns or fewer and needs a tile for every CU: 200 rows of the second, 128 tiles, 154 / 130; 300 rows, 256 tiles, 145 / 186.
+//   * A down launch of fewer tiles than CUs, 96 rows or more and a long K: halves of K (one expert of 3584 x 20480, 200 / 1000 rows 113 / 62,
+//     127 / 94; of 2048 x 2048, 500 rows 22 / 15; but 64 rows of the former 45 / 48, and 130 rows of the second layer, 256 tiles, 116 / 117).
 //   * Few tiles: up to 256 rows by 32 columns per wave, each wave of a tile then multiplies as little as it can and an
 //     expert's weights are read once: fourth, 40 tokens 11.4 / 12.4; with a long K also when there are more tiles, since a tile's
 //     time is what counts (down, 75 rows of the second 98 / 126).  But 90 experts of 768 x 768, 26 rows 42 / 30.
@@ -291,6 +357,8 @@ static I8Choice choose_i8(const hmoe_layer_desc& d, int n_rows, bool gate_up) {
   const bool far = 3l * d.hidden * d.ffn * d.n_experts > (256l << 20);
   const long walk_tiles = (n_rows / 224 + busy) * ((n_total + 255) / 256);
   if (per_expert >= (gate_up ? 60 : 96) && k_steps >= 6 + k_steps % 2 && (gate_up || walk_tiles >= 256)) return {I8_WALK, far && per_expert <= 224};
+  if (!gate_up && k_steps % 4 == 0 && K >= 2048 && per_expert >= 96 && (n_rows / 160 + busy) * ((n_total + 127) / 128) <= 256)
+    return {I8_SPLIT, false};
   const long tiles = (n_rows / 128 + busy) * ((n_total + 255) / 256);
   if (tiles <= 128 || (tiles <= 320 && K >= 4096)) return {I8_FIT256, far && per_expert <= 192};
   return {I8_FIT4, far && per_expert <= 96};
@@ -305,14 +373,15 @@ int launch_ffn_tiled_i8(const FfnArgs& a) {
   const bf16_t* codes = (const bf16_t*)((const char*)a.h + w.codes);
   const float* scales = (const float*)((const char*)a.h + w.scales);
   I8Choice gate_up = choose_i8(d, a.n_rows, true), down = choose_i8(d, a.n_rows, false);
-  if (const char* env = getenv("HMOE_I8_TILES")) {  // tuning and tests: "<gate/up><down>", 0 .. 2 the shapes, 3 .. 5 the same past the caches
-    auto forced = [](char c, int k, I8Choice otherwise) {
+  if (const char* env = getenv("HMOE_I8_TILES")) {  // tuning and tests: "<gate/up><down>", 0 .. 2 the shapes, 3 .. 5 the same past the caches, 6 and 7 down in halves of K
+    auto forced = [&](char c, int k, I8Choice otherwise, bool is_down) {
       const int v = c - '0';
+      if (v == 6 || v == 7) return is_down && k / 128 % 4 == 0 ? I8Choice{I8_SPLIT, v == 7} : otherwise;
       if (v < 0 || v > 5 || (v % 3 == I8_WALK && k / 128 < 6 + k / 128 % 2)) return otherwise;
       return I8Choice{v % 3, v >= 3};
     };
-    gate_up = forced(env[0], d.hidden, gate_up);
-    if (env[0]) down = forced(env[1], d.ffn, down);
+    gate_up = forced(env[0], d.hidden, gate_up, false);
+    if (env[0]) down = forced(env[1], d.ffn, down, true);
   }
   if (i8_shares_rows(a)) {
     launch_quantize_shared_x_i8(a);

@@ -269,6 +269,19 @@ struct StreamTile {
     issue_prologue(a_src, b_src, lds0, wave, k_steps, ring);
     steps(a_src, b_src, lds, wave, lane, k_steps, ring, acc);
   }
+  // ... by a set of waves of a larger block, for an even number of steps: tid is the thread's number in the set, lds the set's
+  // own.  (The barriers are the block's: every set takes as many steps.)
+  static __device__ __forceinline__ void mainloop_of_set(const TiledCtx& c, const bf16_t* __restrict__ in, const TileLoc& loc, int k_begin,
+                                                         int k_steps, u32x4* lds, Acc& acc, int tid) {
+    const int lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)lds;
+    const u32x4* a_src[A_OPS];
+    const u32x4* b_src[FN];
+    set_sources(c, in, loc, loc.mt * MSTRIDE, k_begin, wave, lane, a_src, b_src);
+    u32x4 ring[DB][FN];
+    issue_prologue(a_src, b_src, lds0, wave, k_steps, ring);
+    steps<true>(a_src, b_src, lds, wave, lane, k_steps, ring, acc);
+  }
 
   // fragment i (rows 32 i ..) of k-substep kk of a ring stage, for the lane that owns (half, col) of the operand
   static __device__ __forceinline__ u32x4 read_fragment(const u32x4* lds, int stage, int kk, int i, int half, int col) {
@@ -336,7 +349,8 @@ struct StreamTile {
 
   // The K loop of a tile whose prologue has been issued (by this thread, into `ring` and the first SA-1 stages).
   // On return every vector-memory operation of the thread has completed.
-  template <int NA>
+  // EVEN: k_steps is even, and the ring holds two steps.
+  template <bool EVEN = false, int NA>
   static __device__ __forceinline__ void steps(const u32x4* (&a_src)[NA], const u32x4* (&b_src)[FN], u32x4* lds, int wave,
                                                int lane, int k_steps, u32x4 (&ring)[DB][FN], Acc& acc) {
     const int half = lane / 32, col = lane % 32;
@@ -424,6 +438,14 @@ struct StreamTile {
         k_step(t + 1, std::integral_constant<int, 1>{});
       }
       if (t < k_steps) k_step(t, std::integral_constant<int, 0>{});
+    } else if constexpr (EVEN) {
+      static_assert(DB / KK == 2, "");
+      int t = 0;
+      do {
+        k_step(t, std::integral_constant<int, 0>{});
+        k_step(t + 1, std::integral_constant<int, 1>{});
+        t += 2;
+      } while (t < k_steps);
     } else {
       for (int t = 0; t < k_steps; t += DB / KK) {
         k_step(t, std::integral_constant<int, 0>{});

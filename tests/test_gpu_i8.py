@@ -431,3 +431,18 @@ def test_two_calls_at_once(hm):
             assert torch.equal(o.view(torch.int16), want[i].view(torch.int16))
     for _, _, layer in made:
         layer.close()
+
+
+@pytest.mark.parametrize("tiles", ["06", "07"])
+@pytest.mark.parametrize("hidden,ffn,counts", [(640, 512, [1, 160, 161, 0, 320, 33]), (128, 4608, [130, 97, 64]), (1152, 1024, [31, 500, 0, 128])])
+def test_down_in_two_halves_of_k(hm, monkeypatch, tiles, hidden, ffn, counts):
+    """Two sets of waves per tile (2, 18 and 4 K steps each): the bits of the other tile shapes."""
+    say("i8 split", tiles, hidden, ffn, counts)
+    d, experts, layer = make(hm, hidden, ffn, len(counts), 1, hidden, distinct=2)
+    A = sum(counts)
+    args = (hm, d, layer, to_device(rows_of(14, A, hidden)), to_device(offsets_of(counts)), A, TILED)
+    monkeypatch.setenv("HMOE_I8_TILES", "00")
+    want = grouped(*args)
+    monkeypatch.setenv("HMOE_I8_TILES", tiles)
+    assert torch.equal(grouped(*args).view(torch.int16), want.view(torch.int16))
+    layer.close()
