@@ -377,7 +377,7 @@ int32_t hmoe_combine(const hmoe_layer_desc* desc, const void* o_perm, const int3
  * hmoe_permute_backward: the gradient of hmoe_permute's row gather (and of the gather inside the FFN calls):
  *     dx[t] = sum_{j<K} d_x_perm[inv_perm[t*K + j]] (+ add[t])
  *   j in ascending order, then `add` [T, H] (or NULL: what reaches x on other ways, the shared experts' gradient say);
- *   fp32 accumulation, one rounding.  dx may be `add` itself.
+ *   fp32 accumulation, one rounding.  dx may be `add` itself.  An assignment without a row (as above) adds nothing.
  *
  * hmoe_route_backward: the gradient of hmoe_route's softmax over the chosen logits (the choice itself has none):
  *     d_logits[t, topk_idx[t, j]] = topk_w[t, j] * (d_topk_w[t, j] - sum_i topk_w[t, i] * d_topk_w[t, i]), other entries 0

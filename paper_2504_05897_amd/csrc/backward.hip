@@ -589,9 +589,9 @@ static DwPlan dw_plan(const hmoe_layer_desc& d, int T) {
   p.slices = (d.hidden + cols - 1) / cols;
   p.tiles = (d.n_experts + 63) / 64;
   const long blocks = (long)p.slices * p.tiles;
-  p.most = T <= SMALL_TOKENS ? 1 : (int)std::max(1l, std::min(256 / blocks, (long)(T + 255) / 256));
-  p.chunk_tokens = std::max(1, ((T + p.most - 1) / p.most + 255) / 256 * 256);
-  p.chunks = std::max(1, (T + p.chunk_tokens - 1) / p.chunk_tokens);
+  p.most = T <= SMALL_TOKENS ? 1 : (int)std::max(1l, std::min(256 / blocks, (T + 255l) / 256));
+  p.chunk_tokens = (int)std::min(0x7fffff00l, std::max(256l, (T + p.most - 1l) / p.most + 255) / 256 * 256);
+  p.chunks = (int)std::max(1l, ((long)T + p.chunk_tokens - 1) / p.chunk_tokens);
   return p;
 }
 

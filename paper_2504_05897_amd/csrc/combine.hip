@@ -36,7 +36,7 @@ __device__ __forceinline__ void combine_store(uint4* y, const float (&acc)[8]) {
 __device__ __forceinline__ void combine_store(float4* y, const float (&acc)[4]) { *y = make_float4(acc[0], acc[1], acc[2], acc[3]); }
 
 // VEC: 16 bytes, N elements.  K: experts per token (exact up to 8), or 8 at a time of top_k.  STREAM: non-temporal loads.
-// WEIGHTED: by topk_w, else every weight is 1.  (y may be o_shared, which a thread reads before it stores in the same place.)
+// WEIGHTED: by topk_w, else every weight is 1 and an assignment whose row lies outside the T * top_k adds nothing.  (y may be o_shared, which a thread reads before it stores in the same place.)
 template <class VEC, int N, int K, bool EXACT, bool SHARED, bool STREAM, bool WEIGHTED>
 __global__ __launch_bounds__(256) void combine_kernel(const VEC* __restrict__ o_perm, const int32_t* __restrict__ inv_perm,
                                                       const float* __restrict__ topk_w, const VEC* o_shared, int top_k,
@@ -55,8 +55,11 @@ __global__ __launch_bounds__(256) void combine_kernel(const VEC* __restrict__ o_
     VEC v[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      const VEC* row = o_perm + (long)rows[EXACT ? j : min(j0 + j, top_k - 1)] * row_vec + c;
+      const int p = rows[EXACT ? j : min(j0 + j, top_k - 1)];
+      const bool has_row = WEIGHTED || (unsigned)p < gridDim.x * (EXACT ? K : top_k);
+      const VEC* row = o_perm + (long)(has_row ? p : 0) * row_vec + c;
       v[j] = STREAM ? __builtin_bit_cast(VEC, __builtin_nontemporal_load((const u32x4*)row)) : *row;
+      if (!has_row) v[j] = VEC{};
     }
 #pragma unroll
     for (int j = 0; j < K; ++j)
@@ -105,8 +108,11 @@ __global__ __launch_bounds__(256) void combine_f32_kernel(const float* __restric
   const long t = blockIdx.x;
   for (int c = threadIdx.x; c < hidden; c += blockDim.x) {
     float acc = 0.0f;
-    for (int j = 0; j < top_k; ++j)
-      acc += (topk_w ? topk_w[t * top_k + j] : 1.0f) * o_perm[(long)inv_perm[t * top_k + j] * hidden + c];
+    for (int j = 0; j < top_k; ++j) {
+      const int p = inv_perm[t * top_k + j];
+      if (topk_w) acc += topk_w[t * top_k + j] * o_perm[(long)p * hidden + c];
+      else if ((unsigned)p < gridDim.x * top_k) acc += o_perm[(long)p * hidden + c];
+    }
     if (o_shared) acc += o_shared[t * hidden + c];
     y[t * hidden + c] = acc;
   }

@@ -356,3 +356,26 @@ def test_router_backward_of_large_batches(hm, dtype, T, H, E):
     torch.cuda.synchronize()
     ref = go.router_backward(xv, wv, dv)[0]
     assert (np.abs(to_host_f32(alone) - ref) <= p.step * (np.abs(ref) + slack) + slack).all()
+
+
+@pytest.mark.parametrize("dtype,T,H,K", [("bf16", 6, 64, 2), ("bf16", 7, 72, 11), ("f32", 6, 64, 3), ("f32", 5, 37, 2)])
+def test_permute_backward_of_assignments_without_a_row(hm, dtype, T, H, K):
+    """An assignment outside [0, T*K) adds nothing, whatever row 0 holds; a token may have none left."""
+    say("permute backward, rows missing", dtype, T, H, K)
+    p = Problem(hm, dtype, T, H, 16, K, seed=4)
+    inv = p.inv.copy()
+    inv[K:2 * K] = -1
+    inv[-1] = T * K
+    rows = np.array(p.value(p.dx_perm))
+    rows[p.inv[K:2 * K]] = 0.0
+    rows[p.inv[-1]] = 0.0
+    ref = go.permute_backward(rows, p.inv, T, None)
+    slack = (K + 1) * U * np.abs(rows)[p.inv].reshape(T, K, H).sum(1)
+    dx_perm = to_device(p.dx_perm)
+    unnamed = sorted({int(r) for r in p.inv[K:2 * K]} | {int(p.inv[-1])})
+    dx_perm[unnamed] = float("inf")
+    dx = p.empty(T, H)
+    hm.hmoe_permute_backward(p.desc, dx_perm, to_device(inv), T, None, dx)
+    torch.cuda.synchronize()
+    got = to_host_f32(dx)
+    assert (np.abs(got - ref) <= p.step * (np.abs(ref) + slack) + slack).all() and (got[1] == 0).all()
