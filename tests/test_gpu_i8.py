@@ -446,3 +446,18 @@ def test_down_in_two_halves_of_k(hm, monkeypatch, tiles, hidden, ffn, counts):
     monkeypatch.setenv("HMOE_I8_TILES", tiles)
     assert torch.equal(grouped(*args).view(torch.int16), want.view(torch.int16))
     layer.close()
+
+
+@pytest.mark.parametrize("hidden,ffn", [(128, 14336), (14336, 128)])
+def test_codes_beyond_32_bits_of_offset(hm, hidden, ffn):
+    """More than 4 GiB of codes (of h, of tokens): every repetition of the same rows has the bits of a call over one of them."""
+    say("i8 far rows", hidden, ffn)
+    n, times = 1009, 308
+    assert n * times * 14336 > 1 << 32
+    d, experts, layer = make(hm, hidden, ffn, 1, 1, 21)
+    x = to_device(rows_of(15, n, hidden))
+    want = grouped(hm, d, layer, x, to_device(offsets_of([n])), n, TILED)
+    A = n * times
+    o = grouped(hm, d, layer, x.repeat(times, 1), to_device(offsets_of([A])), A, TILED)
+    assert (o.view(torch.int16).view(times, n, hidden) == want.view(torch.int16)).all()
+    layer.close()
