@@ -61,7 +61,7 @@ using TileI8 = StreamTile<GATEUP, BM, NWV, 4, NT, RING, FM, FN, false, false, St
 template <bool GATEUP, int NWV, bool NT, class OUT>
 __global__ __launch_bounds__(64 * NWV, 2) void ffn_tile_i8_kernel(TiledCtx c, const bf16_t* __restrict__ in,
                                                                 const float* __restrict__ row_scales, OUT* __restrict__ out) {
-  constexpr int RING = NWV == 4 ? 4 : 8;
+  constexpr int RING = 4;
   typedef TileI8<GATEUP, 128, NWV, NT, RING, 4, 2> FULL;
   __shared__ u32x4 lds[FULL::LDS_VEC];
   TileLoc loc;
