@@ -309,3 +309,107 @@ def find_wait_count_errors(asm_text: str) -> List[str]:
         elif name:
             lines.append((no, line))
     return found
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# LDS that one wave reads and another writes over.
+#
+# A barrier of the sources is a bare s_barrier: a wave may pass it with reads from LDS still on their way, and nothing then
+# orders those behind the writes that other waves issue after it.  Before a barrier that hands a piece of LDS to its next
+# writer, every read of the old values therefore has to have come back (lgkmcnt).  The scan is linear like the first one: a read
+# that no wait has retired when its wave passes a barrier, with a write to LDS between that barrier and the next one, is
+# reported if its value is used later: a wait behind the barrier comes too late, since other waves may have written by then.  Values that nothing uses are the fragments which the
+# last K step of a tile reads ahead; what those read does not matter.  Copies from global memory into LDS are not looked at: they
+# fill the activation ring, whose stages are handed over by the waits of the K loop.
+_LDS_REGS = re.compile(r"^([va])(?:(\d+)|\[(\d+):(\d+)\])$")
+
+
+def _regs(operand: str) -> Set[Tuple[str, int]]:
+    m = _LDS_REGS.match(operand.split(" ")[0].strip("-|"))
+    if not m:
+        return set()
+    first, last = (int(m.group(2)),) * 2 if m.group(2) else (int(m.group(3)), int(m.group(4)))
+    return {(m.group(1), i) for i in range(first, last + 1)}
+
+
+def _reads_and_writes(text: str) -> Tuple[Set[Tuple[str, int]], Set[Tuple[str, int]]]:
+    """Vector registers that an instruction reads and those that it writes."""
+    op, _, rest = text.partition(" ")
+    ops = [o.strip() for o in _SPLIT.split(rest) if o.strip()] if rest else []
+    loads = op.startswith(("global_load", "flat_load", "buffer_load", "scratch_load")) and "_lds" not in op
+    has_dest = loads or op.startswith(("ds_read", "ds_bpermute", "ds_permute", "ds_swizzle")) or (
+        op.startswith("v_") and not op.startswith(("v_cmp", "v_readfirstlane", "v_readlane")))
+    writes = _regs(ops[0]) if has_dest and ops else set()
+    reads: Set[Tuple[str, int]] = set()
+    for o in (ops[1:] if has_dest else ops):
+        reads |= _regs(o)
+    if op.startswith(("v_fmac", "v_dot", "v_swap", "v_writelane")) or "sdwa" in op:   # (the destination is a source as well)
+        reads |= writes
+    return reads, writes
+
+
+def _scan_lds(name: str, lines: List[Tuple[int, str]]) -> List[str]:
+    found: List[str] = []
+    # what lgkmcnt counts and no wait has retired, oldest first: destination registers (none for scalar loads and LDS writes),
+    # line, index
+    queue: List[dict] = []
+    passed: List[dict] = []   # the reads that the last barrier was passed with
+
+    def used(at: int, regs: Set[Tuple[str, int]]) -> bool:
+        live = set(regs)
+        for _, raw in lines[at + 1:]:
+            text = raw.split(";")[0].strip()
+            if not text or text.endswith(":") or text.startswith("."):
+                continue
+            if text.split(" ")[0] in ("s_branch", "s_endpgm", "s_setpc_b64"):
+                return False
+            reads, writes = _reads_and_writes(text)
+            if reads & live:
+                return True
+            live -= writes
+            if not live:
+                return False
+        return False
+
+    for i, (no, raw) in enumerate(lines):
+        text = raw.split(";")[0].strip()
+        if not text or text.endswith(":") or text.startswith("."):
+            continue
+        op, _, rest = text.partition(" ")
+        if op in ("s_branch", "s_endpgm", "s_setpc_b64"):
+            queue, passed = [], []   # (what follows is another path's start)
+        elif op == "s_waitcnt":
+            m = re.search(r"lgkmcnt\((\d+)\)", rest)
+            if m:
+                n = int(m.group(1))
+                queue = queue[len(queue) - n:] if n and n < len(queue) else queue if n else []
+        elif op == "s_barrier":
+            passed = [q for q in queue if q["dest"]]
+        elif op.startswith("ds_"):
+            if op.startswith(("ds_write", "ds_add", "ds_max", "ds_min", "ds_or", "ds_and")):
+                for q in passed:
+                    if used(q["at"], q["dest"]):
+                        found.append("%s: line %d: %s may overtake the read from LDS of line %d, which had not come back when its wave "
+                                     "passed the barrier between them" % (name, no, op, q["line"]))
+                passed = []
+            queue.append({"dest": _reads_and_writes(text)[1] if op.startswith("ds_read") else set(), "line": no, "at": i})
+        elif op.startswith(("s_load", "s_buffer_load")):
+            queue.append({"dest": set(), "line": no, "at": i})
+    return found
+
+
+def find_lds_overtakes(asm_text: str) -> List[str]:
+    """Scans every function of a device assembly listing for reads from LDS that a write behind a barrier may overtake."""
+    found: List[str] = []
+    name, lines = None, []
+    for no, line in enumerate(asm_text.splitlines(), 1):
+        m = re.match(r"^(_Z\w+):", line)
+        if m:
+            name, lines = m.group(1), []
+        elif line.startswith(".Lfunc_end"):
+            if name:
+                found += _scan_lds(name, lines)
+            name, lines = None, []
+        elif name:
+            lines.append((no, line))
+    return found

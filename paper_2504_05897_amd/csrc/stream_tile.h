@@ -657,6 +657,7 @@ struct StreamTile {
 #pragma unroll
           for (int t = 0; t < 4; ++t) sums[i][j][q * 4 + t] = i8_product(acc[i][j][q * 4 + t], rs[t], col_scales[j]);
       }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // the scales are in registers before the barrier after which others write over them
   }
   // Gate/up with two weight groups per wave and h in fp32: the wave's 32 columns are a whole line, which each store fills
   // for two rows.

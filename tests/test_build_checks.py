@@ -195,3 +195,25 @@ def test_wait_recount_skips_what_is_not_a_loop():
     nested = listing(".LBB0_0:\n" + HAND.replace("v[10:13]", "v[30:33]") + ".LBB0_1:\n" + good + "\ts_cbranch_scc1 .LBB0_1\n"
                      "\tv_mfma_f32_32x32x16_bf16 v[50:65], v[30:33], v[44:47], v[50:65]\n\ts_cbranch_scc1 .LBB0_0\n")
     assert check(nested) == []
+
+
+def test_reads_from_lds_come_back_before_others_write():
+    """The barriers of the hand-scheduled kernels are bare: a wave that passes one with a read from LDS on its way may get what
+    another wave writes behind it.  A wait between the read and the barrier, or a value that nothing uses, is clean."""
+    check = _load("asm_check").find_lds_overtakes
+    read, write, use = "\tds_read_b128 v[10:13], v7\n", "\tds_write_b16 v8, v9\n", "\tv_mul_f32_e32 v20, v11, v21\n"
+    wait, barrier = "\ts_waitcnt lgkmcnt(%d)\n", "\ts_barrier\n"
+    found = check(listing(read + barrier + write + wait % 0 + use))
+    assert len(found) == 1 and "line 4: ds_write_b16 may overtake the read from LDS of line 2" in found[0]
+    assert check(listing(read + wait % 0 + barrier + write + use)) == []
+    assert len(check(listing(read + barrier + wait % 0 + write + use))) == 1      # another wave need not have waited
+    # reads come back in order: one may stay on its way if it is not the one whose value counts
+    other = "\tds_read_b128 v[14:17], v7 offset:16\n"
+    assert check(listing(other + read + wait % 1 + barrier + write + wait % 0 + use)) != []
+    assert check(listing(read + other + wait % 1 + barrier + write + wait % 0 + use)) == []
+    # a fragment read ahead that nothing uses, its registers taken for something else
+    assert check(listing(read + barrier + write + wait % 0 + "\tv_mov_b32_e32 v10, 0\n\tds_read_b96 v[11:13], v7\n" + use)) == []
+    # accumulation registers are registers
+    assert len(check(listing(read.replace("v[10:13]", "a[10:13]") + barrier + write + wait % 0 + "\tv_accvgpr_read_b32 v20, a11\n"))) == 1
+    # no barrier: the wave's own accesses stay in order
+    assert check(listing(read + write + wait % 0 + use)) == []
