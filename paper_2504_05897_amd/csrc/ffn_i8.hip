@@ -57,11 +57,10 @@ __device__ __forceinline__ void quantize_row_wave(const T* __restrict__ row, int
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
   const RowQuant q = row_quant(m);
-  constexpr bool EXACT = sizeof(T) == 2;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     const int k = 8 * (i * 64 + lane);
-    if (k < K) *(uint2*)(out + k) = codes_of<EXACT>(v[i], q);
+    if (k < K) *(uint2*)(out + k) = codes_of(v[i], q);
   }
   if (lane == 0) *scale = q.scale;
 }

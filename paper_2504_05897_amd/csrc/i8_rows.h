@@ -27,11 +27,11 @@ __device__ __forceinline__ uint32_t magnitude_bits(const float (&v)[8]) {
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
   return m;
 }
-// What a row's codes are computed with.  bfloat16 rows: 127 v (exact; scaled by a power of two where it could overflow)
-// divided by amax so that halves are seen as such: the product with the reciprocal, corrected by what it leaves of 127 v.  A
-// quotient that fp32 holds exactly, as every half is, comes out exactly (the correction is then a small multiple of its last
-// bit), and one that is no half is at least 2^-17 of its size away from one.  (A division of the compiler's is ten
-// instructions: 201 million values 158 -> 118 us.)  fp32 rows, whose values fall on halves by accident only: the product alone.
+// What a row's codes are computed with: 127 v (scaled by a power of two where it could overflow) divided by amax and rounded
+// as a division is, so that the code is the one that the format names also where the quotient is half a code or next to it.  The
+// quotient is the product with the reciprocal, corrected once by what it leaves of 127 v: with a reciprocal that is itself
+// refined, which costs a row two instructions, that is the nearest fp32 number.  (A division of the compiler's is ten
+// instructions per value: 201 million values 158 -> 118 us.  Without the correction one code of h in four million is another.)
 struct RowQuant {
   float times, by, inverse, scale;
   bool finite;
@@ -43,12 +43,12 @@ __device__ __forceinline__ RowQuant row_quant(uint32_t amax_bits) {
   const float down = amax > 0x1p100f ? 0x1p-10f : 1.0f;
   q.times = 127.0f * down;
   q.by = amax * down;
-  q.inverse = __builtin_amdgcn_rcpf(q.by);
+  const float near = __builtin_amdgcn_rcpf(q.by);
+  q.inverse = fmaf(fmaf(-near, q.by, 1.0f), near, near);
   q.scale = q.finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
   return q;
 }
 // The code of a value is the low byte of the value + 1.5 * 2^23, which has no bits behind the point (nearest even).
-template <bool EXACT>
 __device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q) {
   uint32_t w[2];
 #pragma unroll
@@ -57,9 +57,8 @@ __device__ __forceinline__ uint2 codes_of(const float (&v)[8], const RowQuant& q
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float y = v[i + k] * q.times;
-      float s = y * q.inverse;
-      if (EXACT) s = fmaf(fmaf(-s, q.by, y), q.inverse, s);
-      b[k] = __float_as_uint(s + 12582912.0f);
+      const float s = y * q.inverse;
+      b[k] = __float_as_uint(fmaf(fmaf(-s, q.by, y), q.inverse, s) + 12582912.0f);
     }
     w[i / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
   }
@@ -94,16 +93,15 @@ __device__ __forceinline__ void own_row_codes(const T* __restrict__ row, int K, 
 #pragma unroll
   for (int w = 0; w < NW; ++w) m = max(m, wave_max[w]);
   const RowQuant q = row_quant(m);
-  constexpr bool EXACT = sizeof(T) == 2;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     const int k = 8 * (i * 64 * NW + tid);
-    if (k < K) *(uint2*)(codes + k) = codes_of<EXACT>(v[i], q);
+    if (k < K) *(uint2*)(codes + k) = codes_of(v[i], q);
   }
   for (int k = 8 * (HELD * 64 * NW + tid); k < K; k += 8 * 64 * NW) {
     float far[8];
     load_8(row + k, far);
-    *(uint2*)(codes + k) = codes_of<EXACT>(far, q);
+    *(uint2*)(codes + k) = codes_of(far, q);
   }
   if (tid == 0) *scale = q.scale;
 }

@@ -461,3 +461,25 @@ def test_codes_beyond_32_bits_of_offset(hm, hidden, ffn):
     o = grouped(hm, d, layer, x.repeat(times, 1), to_device(offsets_of([A])), A, TILED)
     assert (o.view(torch.int16).view(times, n, hidden) == want.view(torch.int16)).all()
     layer.close()
+
+
+@pytest.mark.parametrize("path", [SKINNY, TILED])
+@pytest.mark.parametrize("ffn,rows", [(1408, 2900), (4096, 1100), (4608, 900)])     # rows by waves (two sizes) and by blocks
+def test_codes_of_h_are_those_of_the_division(hm, path, ffn, rows):
+    """Each code of h is rint(127 h / amax) of the h at hand in fp32, halves and their neighbours included.  (The call's workspace
+    holds h first and behind it, at a multiple of 256 bytes, its codes.)"""
+    say("i8 codes of h", path, ffn, rows)
+    d, experts, layer = make(hm, 128, ffn, 1, 1, 23)
+    x, offsets = to_device(rows_of(16, rows, 128)), to_device(offsets_of([rows]))
+    n = hm.hmoe_ffn_workspace_bytes(d, rows)
+    ws, o = torch.zeros(n, dtype=torch.uint8, device=DEV), torch.empty(rows, 128, dtype=torch.bfloat16, device=DEV)
+    hm.hmoe_expert_ffn_grouped(d, layer.cache, x, offsets, rows, None, o, ws, n, path)
+    torch.cuda.synchronize()
+    at = -(-rows * ffn * 4 // 256) * 256
+    h = ws[:rows * ffn * 4].view(torch.float32).view(rows, ffn).cpu().numpy()
+    codes = ws[at:at + rows * ffn].view(torch.int8).view(rows, ffn).cpu().numpy()
+    amax = np.abs(h).max(1, keepdims=True)
+    assert amax.min() > 1e-3 and np.isfinite(h).all()
+    want = np.rint(h * np.float32(127) / amax)
+    assert want.dtype == np.float32 and (codes == want).all(), int((codes != want).sum())
+    layer.close()
