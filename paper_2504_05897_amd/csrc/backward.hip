@@ -131,9 +131,9 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const int32_t* __re
 // a piece of consecutive columns 16 / sizeof(T) * (l % 16) .., of each of the rows that its k block needs, and column i of every
 // lane's piece makes an operand of its own, for the columns {16 / sizeof(T) * n + i}.  A lane's results are then consecutive
 // columns again.
-//   bfloat16 layers: 16x16x32 instructions; d_logits, fp32, goes in as a sum of bfloat16 pieces, each what is left of the value
-//     cut to its upper 8 bits.  Three pieces hold all 24 bits of a value; dx, which is rounded to bfloat16, takes two
-//     (the second rounded: 2^-17 of a term).  The fp32 instruction would take 27 us for each product of 16384 x 64 x 2048.
+//   bfloat16 layers: 16x16x32 instructions; d_logits, fp32, goes in as a sum of three bfloat16 pieces, each what is left of the
+//     value cut to its upper 8 bits: together all 24 bits, so that the products are exact.  (Two would do for a dx that is rounded
+//     to bfloat16, but not where its terms or `add` cancel.)  The fp32 instruction would take 27 us for each product of 16384 x 64 x 2048.
 //   fp32 layers: 16x16x4 fp32 instructions.
 
 // N of 16-bit pairs: operand dwords (rows 2 d, 2 d + 1) of the lower / upper halves of one dword column of eight rows
@@ -204,11 +204,12 @@ __device__ __forceinline__ void w_operands(u32x4 (&w)[8], u32x4 (&op)[8], int e0
 }
 __device__ __forceinline__ void add_experts(f32x4_t (&acc)[8], const f32x4_t& d0, const f32x4_t& d1, const u32x4 (&op)[8]) {
   float v[8] = {d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
-  const u32x4 hi = take_piece(v), lo = round_piece(v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(hi, op[i], acc[i]);
+  for (int piece = 0; piece < 3; ++piece) {
+    const u32x4 a = take_piece(v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(lo, op[i], acc[i]);
+    for (int i = 0; i < 8; ++i) acc[i] = mfma_16x16x32_bf16(a, op[i], acc[i]);
+  }
 }
 // what is added to rows t0 + 4 kblk .. + 4
 __device__ __forceinline__ void load_more(u32x4 (&more)[4], const bf16_t* add, int t0, int kblk, int n_tokens, int hidden, int col_at) {

@@ -379,3 +379,26 @@ def test_permute_backward_of_assignments_without_a_row(hm, dtype, T, H, K):
     torch.cuda.synchronize()
     got = to_host_f32(dx)
     assert (np.abs(got - ref) <= p.step * (np.abs(ref) + slack) + slack).all() and (got[1] == 0).all()
+
+
+@pytest.mark.parametrize("T,H,E", [(40, 144, 3), (300, 272, 40), (2100, 144, 32), (2500, 272, 61), (2100, 128, 97), (2060, 80, 131)])
+def test_router_input_gradient_whose_terms_cancel(hm, T, H, E):
+    """Three gates per token that sum to zero over router rows with a common value in every column: dx is zero, and what the kernel
+    leaves is its own error.  Whole multiples of 2^-22 below 4, so that the values and their sum are exact.  Tolerance: each of the
+    three values goes through at most three additions in fp32, each off by one step (2^-23 of at most the sum of magnitudes,
+    whichever way it rounds), and zeros add nothing."""
+    say("router backward, cancelling", T, H, E)
+    desc = hm.make_desc(H, 128, E, 3, E, hm.HMOE_BF16)
+    rng = np.random.default_rng(T + E)
+    a = np.rint(rng.uniform(-1, 1, (T, 2)) * 2 ** 22) / 2 ** 22
+    values = np.concatenate([a, -a.sum(1, keepdims=True)], 1)
+    d = np.zeros((T, E), np.float32)
+    np.put_along_axis(d, np.argsort(rng.standard_normal((T, E)), axis=1)[:, :3], values.astype(np.float32), 1)
+    assert (d.astype(np.float64).sum(1) == 0).all()
+    w = np.repeat(wl.store(rng.standard_normal((1, H)).astype(np.float32), wl.BF16), E, 0)
+    n = hm.hmoe_router_backward_workspace_bytes(desc, T)
+    ws, dx = torch.empty(n, dtype=torch.uint8, device=DEV), torch.full((T, H), float("nan"), dtype=torch.bfloat16, device=DEV)
+    hm.hmoe_router_backward(desc, None, to_device(w), to_device(d), T, None, dx, None, ws, n)
+    torch.cuda.synchronize()
+    mags = np.abs(d).sum(1, keepdims=True).astype(np.float64) * np.abs(wl.as_f64(w)[:1])
+    assert (np.abs(to_host_f32(dx)) <= 9 * 2 * U * mags * (1 + 2.0 ** -8)).all()
