@@ -387,6 +387,8 @@ int32_t hmoe_combine(const hmoe_layer_desc* desc, const void* o_perm, const int3
  *     dx[t]    = sum_e d_logits[t, e] * w_g[e] (+ add[t])
  *     d_w_g[e] = sum_t d_logits[t, e] * x[t]          fp32
  *   Either result may be NULL, then what only it needs may be NULL too; dx may be `add` itself, no other two may overlap.
+ *   Every bit of d_logits counts; an infinity of d_logits gives what the sums above give.  In bfloat16 layers one of x or w_g may
+ *   give a NaN where its sum is infinite.
  *   workspace: hmoe_router_backward_workspace_bytes(desc, T) bytes of device scratch, 16-byte aligned.
  */
 int32_t hmoe_combine_backward(const hmoe_layer_desc* desc, const void* dy, const void* o_perm, const int32_t* inv_perm,

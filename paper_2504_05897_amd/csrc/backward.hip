@@ -144,14 +144,18 @@ __device__ __forceinline__ void transpose_halves(const uint32_t (&rows)[8], u32x
     upper[d] = __builtin_amdgcn_perm(rows[2 * d + 1], rows[2 * d], 0x07060302u);
   }
 }
-// the next piece of eight values: their upper halves as an operand, which are taken out of the values
+// The next piece of eight values: their upper halves as an operand, which are taken out of the values.  (What is its own upper
+// half leaves nothing, an infinity too, whose difference with itself would be a NaN.)
 __device__ __forceinline__ u32x4 take_piece(float (&v)[8]) {
   u32x4 piece;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
     piece[d] = __builtin_amdgcn_perm(__float_as_uint(v[2 * d + 1]), __float_as_uint(v[2 * d]), 0x07060302u);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+  for (int i = 0; i < 8; ++i) {
+    const float upper = __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+    v[i] = v[i] == upper ? 0.0f : v[i] - upper;
+  }
   return piece;
 }
 __device__ __forceinline__ u32x4 round_piece(const float (&v)[8]) {
@@ -184,8 +188,8 @@ struct DwF32 {
 
 // dx, bfloat16: a wave has 16 tokens x 128 columns (slice) and goes through the experts 32 at a time.
 //
-// W_g rows e .. + 8 of the lane's k block, eight columns from col_at, as operands; rows past the last are zeros: they meet a
-// value of the token's own row, and if that is infinite, so is the token's result already.
+// W_g rows e .. + 8 of the lane's k block, eight columns from col_at, as operands.  Past the last expert both factors are cleared:
+// the clamped loads bring values of other rows there, and of the token's own, and zero times an infinity is none.
 __device__ __forceinline__ void load_w_rows(u32x4 (&w)[8], const bf16_t* __restrict__ w_g, int e, int n_experts, int hidden, int col_at) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) w[k] = *(const u32x4*)(w_g + (size_t)min(e + k, n_experts - 1) * hidden + col_at);
@@ -202,8 +206,15 @@ __device__ __forceinline__ void w_operands(u32x4 (&w)[8], u32x4 (&op)[8], int e0
     transpose_halves(rows, op[2 * p], op[2 * p + 1]);
   }
 }
-__device__ __forceinline__ void add_experts(f32x4_t (&acc)[8], const f32x4_t& d0, const f32x4_t& d1, const u32x4 (&op)[8]) {
+// e0: of the 32 experts at hand
+__device__ __forceinline__ void add_experts(f32x4_t (&acc)[8], const f32x4_t& d0, const f32x4_t& d1, const u32x4 (&op)[8], int e0, int kblk,
+                                            int n_experts) {
   float v[8] = {d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+  if (e0 + 32 > n_experts) {  // uniform
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (e0 + 8 * kblk + i >= n_experts) v[i] = 0.0f;
+  }
 #pragma unroll
   for (int piece = 0; piece < 3; ++piece) {
     const u32x4 a = take_piece(v);
@@ -256,7 +267,7 @@ __device__ __forceinline__ void router_dx_wave(const bf16_t* __restrict__ w_g, c
     load_w_rows(w, w_g, e, n_experts, hidden, col_at);
     const f32x4_t d0 = load_4<WHOLE>(row, e, n_experts), d1 = load_4<WHOLE>(row, e + 4, n_experts);
     w_operands(w, op, e0, kblk, n_experts);
-    add_experts(acc, d0, d1, op);
+    add_experts(acc, d0, d1, op, e0, kblk, n_experts);
   }
   store_dx(acc, more, add != nullptr, dx, t0, kblk, n_tokens, hidden, col);
 }
@@ -301,7 +312,7 @@ __global__ __launch_bounds__(256, EC <= 2 ? 2 : 1) void router_dx_walk_kernel(co
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
-    for (int c = 0; c < EC; ++c) add_experts(acc, now.d[c][0], now.d[c][1], op[c]);
+    for (int c = 0; c < EC; ++c) add_experts(acc, now.d[c][0], now.d[c][1], op[c], 32 * c, kblk, n_experts);
     store_dx(acc, now.more, add != nullptr, dx, t0, kblk, n_tokens, hidden, col);
   }
 }
@@ -322,11 +333,14 @@ __device__ __forceinline__ void router_dx_wave(const float* __restrict__ w_g, co
 #pragma unroll
     for (int s = 0; s < 4; ++s)
       w[s] = load_4<WHOLE>(w_g + (size_t)min(e + s, n_experts - 1) * hidden, col, hidden);
-    const f32x4_t d = load_4<WHOLE>(row, e, n_experts);
+    f32x4_t d = load_4<WHOLE>(row, e, n_experts);
     if (e0 + 16 > n_experts) {  // uniform
 #pragma unroll
       for (int s = 0; s < 4; ++s)
-        if (e + s >= n_experts) w[s] = f32x4_t{0, 0, 0, 0};
+        if (e + s >= n_experts) {  // (both, as above)
+          w[s] = f32x4_t{0, 0, 0, 0};
+          d[s] = 0.0f;
+        }
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s)

@@ -402,3 +402,32 @@ def test_router_input_gradient_whose_terms_cancel(hm, T, H, E):
     torch.cuda.synchronize()
     mags = np.abs(d).sum(1, keepdims=True).astype(np.float64) * np.abs(wl.as_f64(w)[:1])
     assert (np.abs(to_host_f32(dx)) <= 9 * 2 * U * mags * (1 + 2.0 ** -8)).all()
+
+
+@pytest.mark.parametrize("dtype,T,H,E", [("bf16", 40, 64, 6), ("bf16", 2100, 144, 30), ("bf16", 2100, 80, 45), ("bf16", 2060, 80, 100),
+                                         ("bf16", 2060, 80, 131), ("f32", 40, 37, 6), ("f32", 2060, 36, 21)])
+def test_router_backward_of_infinite_gradients(hm, dtype, T, H, E):
+    """An infinity of d_logits gives what the sums give: an infinity with the sign of its product, in its token's dx and its expert's
+    d_w_g, and a NaN where two of them meet with opposite signs.  (The last expert and the last token stand next to what the kernels
+    fill up with.)"""
+    say("router backward, infinite gradients", dtype, T, H, E)
+    p = Problem(hm, dtype, T, H, E, 2, seed=12)
+    xv, wv = p.value(p.x), p.value(p.w_g)
+    assert (xv != 0).all() and (wv != 0).all()
+    d = p.d_logits.copy()
+    at = [(3, 0, np.inf), (7, E - 1, -np.inf), (T - 1, 1, np.inf), (11, 2, np.inf), (11, 4, -np.inf), (20, E - 1, np.inf), (21, 1, -np.inf)]
+    for t, e, v in at:
+        d[t, e] = v
+    n = hm.hmoe_router_backward_workspace_bytes(p.desc, T)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    dx, d_w = p.empty(T, H), p.empty(E, H, dtype=torch.float32)
+    hm.hmoe_router_backward(p.desc, to_device(p.x), to_device(p.w_g), to_device(d), T, None, dx, d_w, ws, n)
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        ref_dx = np.stack([(d[t].astype(np.float64)[:, None] * wv).sum(0) for t in sorted({t for t, _, _ in at})])
+        ref_dw = np.stack([(d[:, e].astype(np.float64)[:, None] * xv).sum(0) for e in sorted({e for _, e, _ in at})])
+    assert np.isinf(ref_dx).any() and np.isinf(ref_dw).any() and np.isnan(ref_dx).any() and np.isnan(ref_dw).any()
+    dx, d_w = to_host_f32(dx), to_host_f32(d_w)
+    assert np.array_equal(dx[sorted({t for t, _, _ in at})], ref_dx, equal_nan=True)
+    assert np.array_equal(d_w[sorted({e for _, e, _ in at})], ref_dw, equal_nan=True)
+    assert np.isfinite(np.delete(dx, [t for t, _, _ in at], 0)).all() and np.isfinite(np.delete(d_w, [e for _, e, _ in at], 0)).all()
