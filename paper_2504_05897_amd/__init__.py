@@ -591,6 +591,13 @@ class MoELayer:
             self.shared_ws = torch.empty(max(self.shared_ws_bytes, 256), dtype=torch.uint8, device=dev)
         self._call_of = None
         self._layer_call(None)
+        self._pass_tokens = None        # token count of the forward pass that the buffers hold, if they hold a whole one
+        self._captured_passes = set()   # ... of captured passes, any of which a replay may have made the last
+
+    def _passed(self, T: int):
+        self._pass_tokens = T
+        if torch.cuda.is_current_stream_capturing():
+            self._captured_passes.add(T)
 
     def _layer_call(self, bounds) -> LayerCall:
         """Every buffer of a forward pass in one library call.  The attributes are the caller's to replace (a router loaded
@@ -635,6 +642,7 @@ class MoELayer:
         d = self.desc
         T = x.shape[0]
         assert T <= self.max_tokens and x.dtype == self.dt and x.is_contiguous()
+        self._pass_tokens = None
         if all_resident is None:
             all_resident = d.n_slots == d.n_experts
         bounds = None if self.shared_desc is None else self._shared_bounds.data_ptr() + 8 * T
@@ -652,6 +660,7 @@ class MoELayer:
             if not all_resident:
                 self.last_plan = (wave, slot, victim, n_waves.value)
                 self.staged_bytes += int(staged.value)
+            self._passed(T)
             return self.y[:T]
         K, E = d.top_k, d.n_experts
         A = T * K
@@ -709,6 +718,7 @@ class MoELayer:
                                     bounds, None if sd is None else self.o_shared,
                                     None if sd is None else self.shared_ws, 0 if sd is None else self.shared_ws_bytes,
                                     self.y, self.sync, self.sync_bytes, path)
+            self._passed(T)
             return self.y[:T]
         if merged:
             hmoe_expert_ffn_grouped_with_shared(d, self.cache, x, self.perm, self.offsets, A, None, self.o_perm,
@@ -732,6 +742,7 @@ class MoELayer:
                 hmoe_expert_ffn_grouped(self.shared_desc, self.shared_cache, x, bounds, T, None,
                                         self.o_shared, self.shared_ws, self.shared_ws_bytes, path)
         hmoe_combine(d, self.o_perm, self.inv_perm, self.topk_w, o_shared, T, self.y)
+        self._passed(T)
         return self.y[:T]
 
     # -- training the router ----------------------------------------------------------------
@@ -739,11 +750,16 @@ class MoELayer:
         """Gradient of the last forward pass on ``x`` [T, H] with respect to the router, from ``dy`` = dL/dy [T, H] (layer dtype),
         over experts that stay as they are: the weighted sum's, the gates' and the router product's gradients in a row.
 
+        The pass's routing and expert outputs are taken from the layer's buffers: x has to be the batch of the last pass (or of the
+        graph replayed last).  One of another token count than that is refused; another batch of the same size cannot be told.
+
         Returns (d_w_router [E, H] fp32, or None where the layer has no router; d_logits [T, E] fp32), views of internal buffers,
-        valid until the next call.  ``dx`` [T, H] (layer dtype), if given, has the router's part of dL/dx added to it."""
+        valid until the next call.  ``dx`` [T, H] (layer dtype), if given, has the router's part of dL/dx added to it; the experts'
+        part is not computed, so routers below this layer need it from elsewhere."""
         d = self.desc
         T = x.shape[0]
         assert T <= self.max_tokens and x.dtype == self.dt and x.is_contiguous()
+        assert T == self._pass_tokens or T in self._captured_passes, "the last forward pass was of %s tokens, x has %d" % (self._pass_tokens, T)
         assert dy.shape == x.shape and dy.dtype == self.dt and dy.is_contiguous()
         assert dx is None or (dx.shape == x.shape and dx.dtype == self.dt and dx.is_contiguous())
         assert dx is None or self.w_router is not None, "a layer without a router has no input gradient through it"

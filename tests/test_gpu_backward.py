@@ -431,3 +431,38 @@ def test_router_backward_of_infinite_gradients(hm, dtype, T, H, E):
     assert np.array_equal(dx[sorted({t for t, _, _ in at})], ref_dx, equal_nan=True)
     assert np.array_equal(d_w[sorted({e for _, e, _ in at})], ref_dw, equal_nan=True)
     assert np.isfinite(np.delete(dx, [t for t, _, _ in at], 0)).all() and np.isfinite(np.delete(d_w, [e for _, e, _ in at], 0)).all()
+
+
+def test_router_gradient_belongs_to_the_last_pass(hm):
+    """Refused: before a pass, for another token count than the last pass.  Taken: the last pass's, and that of a captured pass,
+    which a replay makes the last one again."""
+    say("router gradient, which pass")
+    shape = wl.small_shape(dtype=wl.BF16, hidden=256, ffn=128, n_experts=8, top_k=2, x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 9, 12)
+    layer = hm.MoELayer(hm.make_desc(256, 128, 8, 2, 8, hm.HMOE_BF16_I8), lay.experts, (), lay.w_router, max_tokens=12)
+    x = to_device(lay.x)
+    dy = torch.randn(12, 256, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3)).bfloat16()
+    with pytest.raises(AssertionError, match="last forward pass"):
+        layer.router_gradient(x, dy)
+    layer.forward(x)
+    want = [v.clone() for v in layer.router_gradient(x, dy)]
+    few = x[:5].contiguous()
+    layer.forward(few)
+    with pytest.raises(AssertionError, match="of 5 tokens, x has 12"):
+        layer.router_gradient(x, dy)
+    layer.router_gradient(few, dy[:5].contiguous())
+    layer.fused = False                                # the separate calls count as well
+    layer.forward(x)
+    layer.router_gradient(x, dy)
+    layer.fused = True
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x)
+    for _ in range(2):
+        layer.forward(few)
+        graph.replay()
+        got = layer.router_gradient(x, dy)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    layer.close()

@@ -98,3 +98,19 @@ def test_bad_arguments_are_refused_on_the_host(hm):
     assert router(by(ok), a[0], a[1], a[2], 4, None, a[3], a[4], a[5], need - 1, None) == hm.HMOE_ERR_WORKSPACE
     assert router(by(ok), a[0], a[1], a[2], 4, None, a[3], a[4], None, need, None) == hm.HMOE_ERR_WORKSPACE
     assert router(by(eight), a[0], a[1], a[2], 4, None, a[3], a[4], a[5], 1 << 30, None) == hm.HMOE_ERR_UNSUPPORTED
+
+
+def test_router_gradient_refuses_a_batch_that_is_not_the_last_pass(hm):
+    """Before anything reaches the library: no pass yet, another token count than the last pass and every captured one."""
+    import torch
+    layer = hm.MoELayer.__new__(hm.MoELayer)
+    layer.cache, layer.desc, layer.dt, layer.max_tokens, layer.w_router = None, hm.make_desc(64, 64, 8, 2, 8, hm.HMOE_F32), torch.float32, 9, None
+    x = torch.zeros(4, 64)
+    for last, captured in ((None, set()), (3, set()), (9, {1, 5})):
+        layer._pass_tokens, layer._captured_passes = last, captured
+        with pytest.raises(AssertionError, match="last forward pass was of %s tokens, x has 4" % last):
+            layer.router_gradient(x, x)
+    layer._pass_tokens, layer._captured_passes = 9, {4}
+    with pytest.raises(AssertionError) as e:     # (accepted: the next check speaks)
+        layer.router_gradient(x, x[:3])
+    assert "last forward pass" not in str(e.value)
