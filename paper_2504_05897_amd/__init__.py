@@ -177,10 +177,16 @@ def _ptr(t) -> Optional[int]:
     return int(t)
 
 
+# The handle of torch.cuda.current_stream() without the Stream object around it (2.7 us a call, most of a wrapper's time); no
+# public name of torch's, so not every version need have it.
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        # the handle of torch.cuda.current_stream(), without the Stream object around it (2.7 us a call, most of a wrapper's time)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if _current_raw_stream is None:
+            return torch.cuda.current_stream().cuda_stream
+        return _current_raw_stream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)

@@ -159,3 +159,12 @@ def test_fused_front_end_refuses_what_hmoe_route_refuses(hm, T, shift):
     rc = hm._lib.hmoe_router_route_permute(ctypes.byref(d), at[0], at[1], T, logits, idx, w, at[5], at[6], at[7], None, at[8],
                                            1 << 30, None)
     assert rc == hm.HMOE_ERR_INVALID_ARG
+
+
+def test_current_stream_without_the_short_cut(hm, monkeypatch):
+    """A torch without the private name of the current stream's handle: the public one is asked."""
+    class Stream:
+        cuda_stream = 4711
+    monkeypatch.setattr(hm, "_current_raw_stream", None)
+    monkeypatch.setattr(hm.torch.cuda, "current_stream", lambda: Stream())
+    assert hm._stream(None) == 4711 and hm._stream(12) == 12
