@@ -483,3 +483,63 @@ def test_codes_of_h_are_those_of_the_division(hm, path, ffn, rows):
     want = np.rint(h * np.float32(127) / amax)
     assert want.dtype == np.float32 and (codes == want).all(), int((codes != want).sum())
     layer.close()
+
+
+@pytest.mark.parametrize("path", [REFERENCE, SKINNY, TILED])
+@pytest.mark.parametrize("rows", [2, 40])                    # (two rows: the decode blocks quantise them themselves)
+@pytest.mark.parametrize("hidden,ffn,gate_up_std,down_std", [
+    (128, 128, 2.0 ** -98, 1.0),              # tokens near the end of the range, h of 2^60
+    (4224, 128, 2.0 ** -98, 1.0),             # rows that a whole block quantises
+    (128, 128, 2.0 ** -68, 2.0 ** -20),       # h above 2^100 as well: 127 h would be infinite
+    (128, 4224, 2.0 ** -68, 2.0 ** -20),
+])
+def test_codes_of_rows_above_2_to_the_100(hm, path, rows, hidden, ffn, gate_up_std, down_std):
+    """Rows whose 127 v is beyond fp32, of tokens and of h, under weights whose codes are not zero."""
+    say("i8 rows above 2^100", path, rows, hidden, ffn)
+    rng = np.random.default_rng(hidden + ffn)
+    draw = lambda std, *s: wl.store((rng.standard_normal(s) * std).astype(np.float32), wl.BF16)
+    w = draw(gate_up_std, ffn, hidden), draw(gate_up_std, ffn, hidden), draw(down_std, hidden, ffn)
+    layer = hm.MoELayer(hm.make_desc(hidden, ffn, 1, 1, 1, hm.HMOE_BF16_I8), [w], (), None, max_tokens=1, host_copies=False)
+    x = draw(6e37, rows, hidden)
+    assert np.isfinite(wl.as_f64(x)).all() and 127 * np.abs(wl.as_f64(x)).max() > np.finfo(np.float32).max
+    o = to_host_f32(grouped(hm, layer.desc, layer, to_device(x), to_device(offsets_of([rows])), rows, path))
+    with np.errstate(over="ignore"):
+        ref, slack = i8.expert_ffn(wl.as_f64(x), *(wl.as_f64(m) for m in w))
+    assert np.abs(ref).max() > 2.0 ** 60 and np.isfinite(o).all()
+    assert (np.abs(o - ref) <= slack + 2.0 ** -8 * (np.abs(ref) + slack)).all()
+    layer.close()
+
+
+@pytest.mark.parametrize("ffn,rows,path", [(2048, 95, TILED), (2048, 96, TILED), (2048, 200, TILED), (2048, 300, 0), (2176, 200, TILED),
+                                           (1920, 200, TILED), (2560, 1000, 0)])
+def test_down_launches_around_the_rule_for_halves_of_k(hm, ffn, rows, path):
+    """What the prefill kernels choose by themselves for one expert: a long F in multiples of four K steps and 96 rows take two
+    sets of waves per tile, fewer rows and other lengths do not."""
+    say("i8 split rule", ffn, rows, path)
+    d, experts, layer = make(hm, 256, ffn, 1, 1, 27)
+    x = rows_of(18, rows, 256)
+    o = to_host_f32(grouped(hm, d, layer, to_device(x), to_device(offsets_of([rows])), rows, path))
+    some = np.unique(np.r_[0:4, rows // 2:rows // 2 + 4, rows - 4:rows])
+    check_rows(o[some], x[some], offsets_of([len(some)]), experts)
+    assert np.isfinite(o).all()
+    layer.close()
+
+
+@pytest.mark.parametrize("path", [REFERENCE, SKINNY, TILED])
+@pytest.mark.parametrize("counts", [[4, 9, 0, 40, 2], [1, 2, 1, 0, 1]])        # (the second: rows quantised by the decode blocks)
+def test_every_resident_expert_where_one_is_not(hm, path, counts):
+    """A call over all experts, one of them evicted: the others' rows are right, its own and those behind the last stay as they are."""
+    say("i8 one expert not resident", path, counts)
+    d, experts, layer = make(hm, 256, 256, len(counts), 1, 9)
+    offsets = offsets_of(counts)
+    A, n_rows = int(offsets[-1]), int(offsets[-1]) + 5
+    x = rows_of(3, A, 256)
+    hm.hmoe_cache_evict(layer.cache, 1)
+    o = torch.full((n_rows, 256), 7.0, dtype=torch.bfloat16, device=DEV)
+    x_dev = torch.cat([to_device(x), torch.full((5, 256), float("nan"), dtype=torch.bfloat16, device=DEV)])
+    grouped(hm, d, layer, x_dev, to_device(offsets), n_rows, path, o=o)
+    got, resident = to_host_f32(o), [0 if e == 1 else n for e, n in enumerate(counts)]
+    keep = np.concatenate([np.arange(offsets[e], offsets[e + 1]) for e in range(len(counts)) if e != 1])
+    check_rows(got[keep], x[keep], offsets_of(resident), experts)
+    assert (np.delete(got, keep, 0) == 7.0).all()
+    layer.close()
