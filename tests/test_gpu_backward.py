@@ -466,3 +466,79 @@ def test_router_gradient_belongs_to_the_last_pass(hm):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     layer.close()
+
+
+@pytest.mark.parametrize("dtype,T,H,K,times", [("bf16", 700, 2048, 6, 4), ("bf16", 500, 2048, 9, 4), ("bf16", 900, 1928, 2, 10),
+                                               ("f32", 350, 2052, 6, 4)])
+def test_gradients_of_batches_beyond_the_caches(hm, dtype, T, H, K, times):
+    """Rows of 64 MiB and more go past the caches.  Every repetition of a batch's tokens, each with rows of its own, has the bits of
+    a call over the batch alone, whose kernels keep them."""
+    say("gradients past the caches", dtype, T, H, K)
+    p = Problem(hm, dtype, T, H, 16, K, seed=14)
+    A, elem = T * K, 2 if p.bf16 else 4
+    assert A * H * elem < 64 << 20 and (T + A) * H * elem < 64 << 20 <= times * A * H * elem
+    dy, o, dxp, inv, w, add = (to_device(a) for a in (p.dy, p.o, p.dx_perm, p.inv, p.w, p.add))
+    d_o, d_w, dx = p.empty(A, H), p.empty(T, K, dtype=torch.float32), p.empty(T, H)
+    hm.hmoe_combine_backward(p.desc, dy, o, inv, w, T, d_o, d_w)
+    hm.hmoe_permute_backward(p.desc, dxp, inv, T, None, dx)
+    dx_add = p.empty(T, H)
+    hm.hmoe_permute_backward(p.desc, dxp, inv, T, add, dx_add)
+    torch.cuda.synchronize()
+    first = np.stack([(p.value(p.dy)[t] * p.value(p.o)[p.inv[t * K:(t + 1) * K]]).sum(1) for t in range(9)])
+    mags = np.stack([np.abs(p.value(p.dy)[t] * p.value(p.o)[p.inv[t * K:(t + 1) * K]]).sum(1) for t in range(9)])
+    assert (np.abs(d_w[:9].cpu().numpy() - first) <= (H + 1) * U * mags).all()
+
+    many = lambda v: v.repeat(times, *[1] * (v.dim() - 1))
+    far = (inv[None] + A * torch.arange(times, dtype=torch.int32, device=DEV)[:, None]).view(-1)
+    bits = lambda v: v.view(torch.int16 if v.dtype == torch.bfloat16 else torch.int32)
+    same = lambda got, want: (bits(got).view(times, *want.shape) == bits(want)).all()
+    big_o, big_w = p.empty(times * A, H), p.empty(times * T, K, dtype=torch.float32)
+    o_many, dy_many, w_many, dxp_many = many(o), many(dy), many(w), many(dxp)
+    hm.hmoe_combine_backward(p.desc, dy_many, o_many, far, w_many, times * T, big_o, big_w)
+    only_w = p.empty(times * T, K, dtype=torch.float32)
+    hm.hmoe_combine_backward(p.desc, dy_many, o_many, far, None, times * T, None, only_w)
+    torch.cuda.synchronize()
+    assert same(big_o, d_o) and same(big_w, d_w) and same(only_w, d_w)
+    big_o.fill_(float("nan"))
+    hm.hmoe_combine_backward(p.desc, dy_many, None, far, w_many, times * T, big_o, None)
+    in_place = p.empty(times * T, K, dtype=torch.float32)
+    hm.hmoe_combine_backward(p.desc, dy_many, o_many, far, w_many, times * T, o_many, in_place)     # in the place of the rows
+    torch.cuda.synchronize()
+    assert same(big_o, d_o) and same(o_many, d_o) and same(in_place, d_w)
+    big_x, big_add = p.empty(times * T, H), many(add)
+    hm.hmoe_permute_backward(p.desc, dxp_many, far, times * T, None, big_x)
+    hm.hmoe_permute_backward(p.desc, dxp_many, far, times * T, big_add, big_add)                    # in the place of what is added
+    torch.cuda.synchronize()
+    assert same(big_x, dx) and same(big_add, dx_add)
+
+
+@pytest.mark.parametrize("dtype,n_slots", [("i8", 8), ("i8", 3), ("bf16", 5)])
+def test_router_gradient_of_a_large_batch_and_a_partial_cache(hm, dtype, n_slots):
+    """Beyond the batches whose router gradient is one launch, with experts staged wave by wave: against the oracle's chain over the
+    pass's own choice and expert outputs (bounds as in test_router_gradient_of_a_layer, dx's products exact)."""
+    say("router gradient, large", dtype, n_slots)
+    T, H, E, K = 2300, 256, 8, 2
+    shape = wl.small_shape(dtype=wl.BF16, hidden=H, ffn=128, n_experts=E, top_k=K, n_slots=n_slots, x_mode="rmsnorm")
+    lay = wl.make_layer(shape, 17, T)
+    kind = hm.HMOE_BF16_I8 if dtype == "i8" else hm.HMOE_BF16
+    layer = hm.MoELayer(hm.make_desc(H, 128, E, K, n_slots, kind), lay.experts, (), lay.w_router, max_tokens=T)
+    x = to_device(lay.x)
+    dy = layer.forward(x).clone()                     # the gradient of 1/2 |y|^2
+    seen = torch.randn(T, H, device=DEV, generator=torch.Generator(device=DEV).manual_seed(2)).bfloat16()
+    dx = seen.clone()
+    d_w, d_logits = layer.router_gradient(x, dy, dx)
+    torch.cuda.synchronize()
+    assert n_slots == E or layer.last_plan[3] > 1
+    f = lambda t: t.double().cpu().numpy()
+    idx, w, inv, o = layer.topk_idx.cpu().numpy(), f(layer.topk_w), layer.inv_perm.cpu().numpy(), f(layer.o_perm)
+    _, d_topk = go.combine_backward(f(dy), o, inv, w)
+    ref_l = go.route_backward(idx, w, d_topk, E)
+    ref_dx, ref_w = go.router_backward(f(x), wl.as_f64(lay.w_router), ref_l, f(seen))
+    mags = np.abs(f(dy)[:, None] * o[inv].reshape(T, K, H)).sum(2).max(1, keepdims=True)
+    slack = 2 * (H + 8) * U * mags * (ref_l != 0)
+    assert (np.abs(f(d_logits) - ref_l) <= slack).all()
+    xa, wa = np.abs(f(x)), np.abs(wl.as_f64(lay.w_router))
+    assert (np.abs(f(d_w) - ref_w) <= slack.T @ xa + (T + 2) * U * (np.abs(ref_l).T @ xa)).all()
+    slack_x = slack @ wa + 3 * (E + 2) * 2 * U * (np.abs(ref_l) @ wa + np.abs(f(seen)))    # three pieces of each term, either rounding
+    assert (np.abs(f(dx) - ref_dx) <= slack_x + 2.0 ** -8 * (np.abs(ref_dx) + slack_x)).all()
+    layer.close()
