@@ -591,7 +591,10 @@ __global__ __launch_bounds__(256) void router_dw_sum_kernel(const float* __restr
   }
 }
 
-// Up to this many tokens one launch does everything (1003 tokens, 64 experts of 2048: 8.4 us, the launches of larger batches 5.1 + 12.9 + 4.2).
+// Up to this many tokens one launch does everything (us, this launch / those of larger batches, bfloat16: 64 experts of 2048, 1003 and
+// 2048 tokens 7.0 / 14.8, 10.6 / 18.7; 160 of 4096 20.3 / 24.0, 33.2 / 34.5; 256 of 4096 23.3 / 27.2, 43.3 / 42.3, but 256 tokens 16.5 / 14.9).
+// In fp32, with twice the bytes and steps half as long, the two meet earlier (64 of 2048 16.5 / 17.7, 32.1 / 24.9; 256 of 4096, 64 and 256
+// tokens 12.8 / 13.7, 25.5 / 17.7, 2048 tokens 139.7 / 95.7): a border that knew the type and the experts would lie lower there.
 constexpr int SMALL_TOKENS = 2048;
 // Beyond: chunks of the tokens in the d_w_g launch, as many as give every CU a block.
 struct DwPlan {
